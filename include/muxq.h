@@ -319,6 +319,36 @@ int muxq_linear_decode_noalloc(const void *X_f16, int M, int K, int ldx, const i
                                const float *s_w, int N, const muxq_params *p, void *Y, int ldy,
                                int out_kind, int32_t *dev_status, void *stream);
 
+/*
+ * What stands between two projections of a transformer block (the paper quantizes the projections and leaves this as it is):
+ *   h = R + alpha * gate (.) post(Y)        the residual stream behind the block whose projection left Y
+ *   x = pre(h)                              the fp16 input of the next muxq_linear
+ *   RMS:    n(v) = v / sqrt(mean(v^2) + eps) * weight + bias
+ *   LAYER:  n(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) * weight + bias
+ *   NONE:   n(v) = v
+ * in one pass, fp32 throughout; h and x are rounded once each, x from the h that is not rounded yet.
+ *   R    [M, ldr] by res_kind (MUXQ_OUT_F16 / MUXQ_OUT_F32), or NULL: 0.  Then res_kind is H's type only.
+ *   Y    [M, ldy] by y_kind, or NULL: h = R (post and gate must then be absent, alpha is not used).  R or Y is given.
+ *   post, pre   host structs, or NULL (NONE).  weight, bias: device, fp32 [D], 16-byte aligned, or NULL (1, 0); NONE takes neither.
+ *        0 < eps < inf.
+ *   gate device, by gate_kind, or NULL (1): [D] with gate_group = 0, or one row of D for every gate_group consecutive token
+ *        rows, [ceil(M / gate_group), ldg] (1: a row for every token; T: one for each of several sequences of T tokens).
+ *   H    [M, ldh] by res_kind, or NULL; may be R itself (same address and pitch).   X [M, ldx] fp16, or NULL.  H or X is given.
+ * H and X overlap nothing else that the call reads or writes (columns of one wider matrix that lie side by side do not overlap).
+ * Rows behind M and columns behind D are left as they are.  D % 8 == 0, D <= 16384; pitches are multiples of 8 (fp16) or 4 (fp32)
+ * elements, all addresses 16-byte aligned.  No workspace.  Everything is read in stream order.  Values beyond the finite ones make
+ * their own row unspecified and no other; h^2 must not leave fp32 (|h| < 1e18).
+ */
+typedef enum { MUXQ_NORM_NONE = 0, MUXQ_NORM_RMS = 1, MUXQ_NORM_LAYER = 2 } muxq_norm_kind;
+typedef struct muxq_norm {
+    int kind; /* muxq_norm_kind */
+    float eps;
+    const float *weight, *bias;
+} muxq_norm;
+int muxq_residual_norm(const void *R, int ldr, int res_kind, const void *Y, int ldy, int y_kind, const muxq_norm *post,
+                       const void *gate, int ldg, int gate_kind, int gate_group, float alpha, const muxq_norm *pre, int M,
+                       int D, void *H, int ldh, void *X_f16, int ldx, void *stream);
+
 /* Synchronizes `stream` and returns the device status word (or MUXQ_ERR_CUDA). */
 int muxq_read_status(const int32_t *dev_status, void *stream);
 

@@ -6,7 +6,7 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -18,13 +18,14 @@ MUXQ_ERR_CUDA, MUXQ_ERR_CAPACITY, MUXQ_ERR_TIMEOUT, MUXQ_ERR_STATIC_LIMIT = 4, 5
 MUXQ_PER_TENSOR, MUXQ_PER_VECTOR = 0, 1
 MUXQ_AUX_SHARED, MUXQ_AUX_OWN = 0, 1
 MUXQ_OUT_F16, MUXQ_OUT_F32, MUXQ_OUT_ACC_I32 = 0, 1, 2
+MUXQ_NORM_NONE, MUXQ_NORM_RMS, MUXQ_NORM_LAYER = 0, 1, 2
 
 EXPORTS = (
     "muxq_default_params", "muxq_aux_cols", "muxq_workspace_bytes", "muxq_small_workspace_bytes",
     "muxq_host_workspace_bytes", "muxq_workspace_init", "muxq_workspace_view", "muxq_detect_outliers", "muxq_build_aux",
     "muxq_quantize", "muxq_gemm", "muxq_linear", "muxq_linear_bias", "muxq_linear_events", "muxq_linear_host",
     "muxq_linear_decode_noalloc", "muxq_int8_mma_peak", "muxq_test_hooks", "muxq_test_late_warps", "muxq_read_status",
-    "muxq_chain_plan_bytes", "muxq_chain_device_bytes", "muxq_chain_build", "muxq_chain_run",
+    "muxq_residual_norm", "muxq_chain_plan_bytes", "muxq_chain_device_bytes", "muxq_chain_build", "muxq_chain_run",
     "muxq_status_string",
 )
 
@@ -101,6 +102,7 @@ def lib() -> ctypes.CDLL:
         L.muxq_int8_mma_peak.argtypes = [i, i, i, vp, vp, vp]; L.muxq_int8_mma_peak.restype = i
         L.muxq_test_hooks.argtypes = [vp]; L.muxq_test_hooks.restype = i
         L.muxq_test_late_warps.argtypes = [ctypes.c_uint32]; L.muxq_test_late_warps.restype = i
+        L.muxq_residual_norm.argtypes = [vp, i, i, vp, i, i, vp, vp, i, i, i, f, vp, i, i, vp, i, vp, i, vp]; L.muxq_residual_norm.restype = i
         L.muxq_chain_plan_bytes.argtypes = [i]; L.muxq_chain_plan_bytes.restype = sz
         L.muxq_chain_device_bytes.argtypes = [vp, i, i]; L.muxq_chain_device_bytes.restype = sz
         L.muxq_chain_build.argtypes = [vp, i, i, pp, i, vp, sz, vp, sz, vp]; L.muxq_chain_build.restype = i
@@ -108,8 +110,9 @@ def lib() -> ctypes.CDLL:
         L.muxq_read_status.argtypes = [vp, vp]; L.muxq_read_status.restype = i
         L.muxq_status_string.argtypes = [i]; L.muxq_status_string.restype = ctypes.c_char_p
         from . import _calls as calls
-        calls.bind(*(ctypes.cast(f, vp).value for f in (L.muxq_linear, L.muxq_linear_bias, L.muxq_quantize)),
-                   torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.float16, torch.float32)
+        at = lambda entry: ctypes.cast(entry, vp).value
+        calls.bind(at(L.muxq_linear), at(L.muxq_linear_bias), at(L.muxq_quantize), torch._C._cuda_getDevice,
+                   torch._C._cuda_getCurrentRawStream, torch.float16, torch.float32, at(L.muxq_residual_norm))
         _calls = calls  # first: a thread that finds _lib set goes on to use it
         _lib = L
     return _lib
@@ -318,6 +321,35 @@ def muxq_int8_mma_peak(mma_n: int, iters: int, ctas: int, ws: Workspace) -> torc
     cycles = torch.zeros(ctas, dtype=torch.int64, device=ws.buf.device)
     _check("muxq_int8_mma_peak", lib().muxq_int8_mma_peak(mma_n, iters, ctas, _ptr(cycles), _ptr(ws.status), _stream()))
     return cycles
+
+
+class Norm(NamedTuple):
+    """A norm over the channels of a token: kind MUXQ_NORM_LAYER or MUXQ_NORM_RMS; weight and bias fp32 [D] (None: 1, 0)."""
+    kind: int
+    weight: Optional[torch.Tensor] = None
+    bias: Optional[torch.Tensor] = None
+    eps: float = 1e-5
+
+
+def muxq_residual_norm(R: Optional[torch.Tensor], Y: Optional[torch.Tensor], pre: Optional[Norm], post: Optional[Norm] = None,
+                       gate: Optional[torch.Tensor] = None, gate_group: int = 1, scale: float = 1.0,
+                       H: Optional[torch.Tensor] = None, X: Optional[torch.Tensor] = None, want_h: bool = True,
+                       want_x: bool = True) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(h, x) with h = R + scale * gate * post(Y) and x = pre(h): the residual stream behind a block whose projection left Y
+    (fp16 or fp32), and the fp16 input of the next muxq_linear.  R and H are fp16 or fp32; H may be R.  gate: [D], or
+    [ceil(M / gate_group), D] with one row for every gate_group consecutive tokens.  Without Y, h is R and is not written; without R,
+    h is the second term alone (fp32 unless H is given).  want_h / want_x = False leave a result out (None)."""
+    some = Y if R is None else R
+    if some is None:
+        raise ValueError("R: R or Y is wanted")
+    if H is None and Y is not None and want_h:
+        H = torch.empty(some.shape, dtype=torch.float32 if R is None else R.dtype, device=some.device)
+    if X is None and want_x:
+        X = torch.empty(some.shape, dtype=torch.float16, device=some.device)
+    rc = _hot().residual_norm(R, Y, pre, post, gate, gate_group, scale, H, X)
+    if rc:
+        raise MuxqError("muxq_residual_norm", rc)
+    return H, X
 
 
 MUXQ_LAYER_WAIT_PREV = 1

@@ -75,6 +75,43 @@ LinearWs linear_ws(int M, int K, int N, const muxq_params *p) {
 
 inline size_t out_elem_bytes(int out_kind) { return out_kind == MUXQ_OUT_F16 ? 2 : 4; }
 
+// A matrix in memory, in bytes.
+struct Span {
+    const void *at;
+    size_t rows, pitch, width;
+};
+Span span(const void *p, int rows, int cols, int ld, int kind) {
+    return Span{p, (size_t)rows, (size_t)ld * out_elem_bytes(kind), (size_t)cols * out_elem_bytes(kind)};
+}
+// Whether two matrices share a byte.  Columns of one wider matrix that lie side by side do not; of two matrices with different
+// pitches whose ranges of addresses meet it is taken that they do.
+bool overlap(const Span &a, const Span &b) {
+    if (!a.at || !b.at) return false;
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.at), b0 = reinterpret_cast<uintptr_t>(b.at);
+    const uintptr_t a1 = a0 + (a.rows - 1) * a.pitch + a.width, b1 = b0 + (b.rows - 1) * b.pitch + b.width;
+    if (a1 <= b0 || b1 <= a0) return false;
+    if (a.pitch != b.pitch || !a.pitch) return true;
+    const size_t d = (size_t)(b0 > a0 ? b0 - a0 : a0 - b0) % a.pitch;  // the later one's column within the earlier one's rows
+    const size_t first = b0 > a0 ? a.width : b.width, second = b0 > a0 ? b.width : a.width;
+    return d < first || d + second > a.pitch;
+}
+bool same_place(const Span &a, const Span &b) { return a.at == b.at && a.pitch == b.pitch && a.width == b.width; }
+
+bool real_kind(int kind) { return kind == MUXQ_OUT_F16 || kind == MUXQ_OUT_F32; }
+bool pitch_ok(int ld, int kind) { return ld % (kind == MUXQ_OUT_F16 ? 8 : 4) == 0; }
+
+// 0, or the code of what is wrong with it
+int norm_of(const muxq_norm *n, NormSpec *out) {
+    *out = NormSpec{MUXQ_NORM_NONE, 1.0f, nullptr, nullptr};
+    if (!n) return MUXQ_OK;
+    if (n->kind < MUXQ_NORM_NONE || n->kind > MUXQ_NORM_LAYER) return MUXQ_ERR_INVALID_ARG;
+    if (n->kind == MUXQ_NORM_NONE) return n->weight || n->bias ? MUXQ_ERR_INVALID_ARG : MUXQ_OK;
+    if (!(n->eps > 0.0f) || !isfinite(n->eps)) return MUXQ_ERR_INVALID_ARG;
+    if (!aligned16(n->weight) || !aligned16(n->bias)) return MUXQ_ERR_UNSUPPORTED;
+    *out = NormSpec{n->kind, n->eps, n->weight, n->bias};
+    return MUXQ_OK;
+}
+
 int cuda_rc(cudaError_t e) { return e == cudaSuccess ? MUXQ_OK : MUXQ_ERR_CUDA; }
 
 }  // namespace
@@ -522,6 +559,42 @@ int muxq_int8_mma_peak(int mma_n, int iters, int ctas, unsigned long long *cycle
     if ((mma_n != 128 && mma_n != 256 && mma_n != 16 && mma_n != 64) || iters < 1 || iters > (1 << 20) || ctas < 1 || !cycles_per_cta)
         return MUXQ_ERR_INVALID_ARG;
     return cuda_rc(launch_mma_peak(mma_n, iters, cycles_per_cta, dev_status, ctas, static_cast<cudaStream_t>(stream)));
+}
+
+int muxq_residual_norm(const void *R, int ldr, int res_kind, const void *Y, int ldy, int y_kind, const muxq_norm *post,
+                       const void *gate, int ldg, int gate_kind, int gate_group, float alpha, const muxq_norm *pre, int M,
+                       int D, void *H, int ldh, void *X, int ldx, void *stream) {
+    ResidualNormArgs a{};
+    if ((!R && !Y) || (!H && !X) || M <= 0 || D <= 0 || !real_kind(res_kind) || (Y && !real_kind(y_kind)) ||
+        (gate && (!real_kind(gate_kind) || gate_group < 0)) || (R && ldr < D) || (Y && ldy < D) || (H && ldh < D) || (X && ldx < D) ||
+        (gate && gate_group && ldg < D) || (Y && !isfinite(alpha)))
+        return MUXQ_ERR_INVALID_ARG;
+    int rc = norm_of(post, &a.post);
+    if (rc == MUXQ_OK) rc = norm_of(pre, &a.pre);
+    if (rc != MUXQ_OK) return rc;
+    if (!Y && (gate || a.post.kind != MUXQ_NORM_NONE)) return MUXQ_ERR_INVALID_ARG;
+    if (D % 8 || D > kNormMaxD || !aligned16(R) || !aligned16(Y) || !aligned16(gate) || !aligned16(H) || !aligned16(X) ||
+        (R && !pitch_ok(ldr, res_kind)) || (Y && !pitch_ok(ldy, y_kind)) || (H && !pitch_ok(ldh, res_kind)) || (X && ldx % 8) ||
+        (gate && gate_group && !pitch_ok(ldg, gate_kind)))
+        return MUXQ_ERR_UNSUPPORTED;
+    const int groups = gate_group ? (int)(((long long)M + gate_group - 1) / gate_group) : 1;
+    const Span r = span(R, M, D, ldr, res_kind), y = span(Y, M, D, ldy, y_kind), g = span(gate, groups, D, gate_group ? ldg : D, gate_kind),
+               h = span(H, M, D, ldh, res_kind), x = span(X, M, D, ldx, MUXQ_OUT_F16);
+    if ((overlap(h, r) && !same_place(h, r)) || overlap(h, y) || overlap(h, g) || overlap(x, r) || overlap(x, y) || overlap(x, g) ||
+        overlap(x, h))
+        return MUXQ_ERR_INVALID_ARG;
+    for (const float *v : {a.post.weight, a.post.bias, a.pre.weight, a.pre.bias}) {
+        const Span w = span(v, 1, D, D, MUXQ_OUT_F32);
+        if (overlap(h, w) || overlap(x, w)) return MUXQ_ERR_INVALID_ARG;
+    }
+    a.R = R; a.ldr = ldr; a.res_f32 = res_kind == MUXQ_OUT_F32;
+    a.Y = Y; a.ldy = ldy; a.y_f32 = Y && y_kind == MUXQ_OUT_F32;
+    a.gate = gate; a.ldg = ldg; a.gate_f32 = gate_kind == MUXQ_OUT_F32; a.gate_group = gate_group;
+    a.alpha = alpha;
+    a.M = M; a.D = D;
+    a.H = H; a.ldh = ldh;
+    a.X = static_cast<__half *>(X); a.ldx = ldx;
+    return cuda_rc(launch_residual_norm(a, static_cast<cudaStream_t>(stream)));
 }
 
 // ---------------------------------------------------------------- lists of decode-shaped layers

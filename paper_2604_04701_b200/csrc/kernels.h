@@ -297,6 +297,29 @@ bool list_map(void *map128, const int8_t *w_q, int N, int K, int ldw);  // write
 uint32_t list_plan(ChainLayer *layers, int n_layers, int M);
 cudaError_t launch_decode_list(const ListArgs &a, cudaStream_t s);
 
+// h = R + alpha * gate (.) post(Y), x = pre(h) (k13_residual_norm.cu)
+struct NormSpec {
+    int kind;            // muxq_norm_kind
+    float eps;
+    const float *weight, *bias;  // [D] or NULL (1, 0)
+};
+struct ResidualNormArgs {
+    const void *R, *Y;   // NULL: zero
+    int ldr, ldy, res_f32, y_f32;
+    NormSpec post, pre;
+    const void *gate;    // NULL: 1
+    int ldg, gate_f32;
+    int gate_group;      // rows that share a row of the gate; 0: all
+    float alpha;
+    int M, D;
+    void *H;             // type of R, or NULL
+    int ldh;
+    __half *X;           // or NULL
+    int ldx;
+};
+constexpr int kNormMaxD = 16384;
+cudaError_t launch_residual_norm(const ResidualNormArgs &a, cudaStream_t s);
+
 cudaError_t launch_mma_peak(int n, int iters, unsigned long long *cycles_out, int32_t *status, int grid,
                             cudaStream_t s);
 

@@ -7,6 +7,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
+#include <string.h>
 
 #include "../../include/muxq.h"
 
@@ -17,11 +18,15 @@ typedef int (*linear_bias_fn)(const void *, int, int, int, const int8_t *, int, 
 typedef int (*quantize_fn)(const void *, int, int, int, const muxq_params *, int, const float *, const int32_t *,
                            const int32_t *, int8_t *, int, int8_t *, int, float *, void *, size_t, void *);
 
+typedef int (*residual_norm_fn)(const void *, int, int, const void *, int, int, const muxq_norm *, const void *, int, int, int, float,
+                                const muxq_norm *, int, int, void *, int, void *, int, void *);
+
 static linear_fn f_linear;
 static linear_bias_fn f_linear_bias;
 static quantize_fn f_quantize;
+static residual_norm_fn f_residual_norm;
 static PyObject *get_device, *raw_stream, *dt_f16, *dt_f32;
-static PyObject *n_data_ptr, *n_shape, *n_stride, *n_dtype, *n_is_cuda, *n_numel, *n_is_contiguous;
+static PyObject *n_data_ptr, *n_shape, *n_stride, *n_dtype, *n_is_cuda, *n_numel, *n_is_contiguous, *n_get_device;
 static PyObject *n_threshold, *n_exp_factor, *n_act_bits, *n_w_bits, *n_gran, *n_aux_scale, *n_max_outliers;
 
 static int tensor_ptr(PyObject *t, void **out) {
@@ -98,16 +103,24 @@ static int params_of(PyObject *p, muxq_params *c) {
                : 0;
 }
 
-/* the stream that is current for the calling thread on the current device */
-static int current_stream(void **out) {
+/* the current device, and the stream that is current for the calling thread on it */
+static int current_place(int *device, void **out) {
     PyObject *dev = PyObject_CallNoArgs(get_device);
     if (!dev) return -1;
     PyObject *s = PyObject_CallOneArg(raw_stream, dev);
-    Py_DECREF(dev);
+    if (as_int(dev, device)) {
+        Py_XDECREF(s);
+        return -1;
+    }
     if (!s) return -1;
     *out = PyLong_AsVoidPtr(s);
     Py_DECREF(s);
     return PyErr_Occurred() ? -1 : 0;
+}
+
+static int current_stream(void **out) {
+    int device;
+    return current_place(&device, out);
 }
 
 static PyObject *stream(PyObject *self, PyObject *unused) {
@@ -182,12 +195,100 @@ static PyObject *quantize_weight(PyObject *self, PyObject *const *a, Py_ssize_t 
     return PyLong_FromLong(rc);
 }
 
-/* bind(muxq_linear, muxq_linear_bias, muxq_quantize, get_device, raw_stream, float16, float32) */
+/* A tensor as an operand, with what is wanted of it checked.  `what` stands in the message. */
+typedef struct {
+    void *ptr;
+    int kind, rows, cols, ld, dim; /* kind: MUXQ_OUT_F16 or MUXQ_OUT_F32; one dimension: rows = 1 */
+} operand;
+static int refuse(const char *what, const char *why) {
+    PyErr_Format(PyExc_ValueError, "%s: %s", what, why);
+    return -1;
+}
+static int operand_of(PyObject *t, const char *what, int device, int dims, operand *o) { /* dims: 1, 2, or 3 for either */
+    int at = -1, second = 0, sa, sb, f16, f32;
+    if (as_int(PyObject_CallMethodNoArgs(t, n_get_device), &at)) return -1;
+    if (at < 0) return refuse(what, "a CUDA tensor is wanted");
+    if (at != device) return refuse(what, "the tensor is on another device than the current one");
+    if ((f16 = has_dtype(t, dt_f16)) < 0 || (f32 = has_dtype(t, dt_f32)) < 0) return -1;
+    if (!f16 && !f32) return refuse(what, "fp16 or fp32 is wanted");
+    o->kind = f16 ? MUXQ_OUT_F16 : MUXQ_OUT_F32;
+    if (shape_of(t, &o->rows, &second, &o->dim) || stride_of(t, &sa, &sb)) return -1;
+    if (o->dim > 2 || !(dims & o->dim)) return refuse(what, "the number of dimensions is not what is wanted");
+    if (o->dim == 1) {
+        second = o->rows;
+        o->rows = 1;
+        sb = sa;
+    }
+    o->cols = second;
+    if (second > 1 && sb != 1) return refuse(what, "unit stride along the last dimension is wanted");
+    o->ld = o->rows == 1 ? o->cols : sa; /* (the stride of a dimension of one says nothing) */
+    return tensor_ptr(t, &o->ptr);
+}
+static int matrix_of(PyObject *t, const char *what, int device, int rows, int cols, operand *o) {
+    if (operand_of(t, what, device, 2, o)) return -1;
+    return o->rows == rows && o->cols == cols ? 0 : refuse(what, "the shape does not fit the other operands");
+}
+static int vector_f32(PyObject *t, const char *what, int device, int len, const float **out) {
+    operand o;
+    *out = NULL;
+    if (t == Py_None) return 0;
+    if (operand_of(t, what, device, 1, &o)) return -1;
+    if (o.kind != MUXQ_OUT_F32 || o.cols != len) return refuse(what, "an fp32 vector of the rows' length is wanted");
+    *out = o.ptr;
+    return 0;
+}
+static int norm_of(PyObject *t, const char *what, int device, int len, muxq_norm *n) { /* (kind, weight, bias, eps) or None */
+    memset(n, 0, sizeof *n);
+    if (t == Py_None) return 0;
+    if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 4) return refuse(what, "a Norm is wanted");
+    if (as_int(Py_NewRef(PyTuple_GET_ITEM(t, 0)), &n->kind)) return -1;
+    n->eps = (float)PyFloat_AsDouble(PyTuple_GET_ITEM(t, 3));
+    if (PyErr_Occurred()) return -1;
+    return vector_f32(PyTuple_GET_ITEM(t, 1), what, device, len, &n->weight) || vector_f32(PyTuple_GET_ITEM(t, 2), what, device, len, &n->bias) ? -1 : 0;
+}
+
+/* residual_norm(R or None, Y or None, pre or None, post or None, gate or None, gate_group, scale, H or None, X or None) -> status code */
+static PyObject *residual_norm(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "residual_norm takes 9 arguments");
+    operand r = {0}, y = {0}, g = {0}, h = {0}, x = {0};
+    muxq_norm pre, post;
+    void *s;
+    int device, group;
+    if (current_place(&device, &s)) return NULL;
+    if (a[0] == Py_None && a[1] == Py_None) return refuse("R", "R or Y is wanted"), NULL;
+    if (operand_of(a[0] != Py_None ? a[0] : a[1], "R", device, 2, &r)) return NULL;
+    const int M = r.rows, D = r.cols;
+    if (a[0] == Py_None) r.ptr = NULL;
+    if ((a[1] != Py_None && matrix_of(a[1], "Y", device, M, D, &y)) || (a[7] != Py_None && matrix_of(a[7], "H", device, M, D, &h)) ||
+        (a[8] != Py_None && matrix_of(a[8], "X", device, M, D, &x)) || norm_of(a[2], "pre", device, D, &pre) ||
+        norm_of(a[3], "post", device, D, &post) || as_int(Py_NewRef(a[5]), &group))
+        return NULL;
+    if (a[7] != Py_None && a[0] != Py_None && h.kind != r.kind) return refuse("H", "the type of R is wanted"), NULL;
+    if (a[8] != Py_None && x.kind != MUXQ_OUT_F16) return refuse("X", "fp16 is wanted"), NULL;
+    if (a[4] != Py_None) {
+        if (operand_of(a[4], "gate", device, 3, &g)) return NULL;
+        if (group < 1) return refuse("gate_group", "at least 1 is wanted"), NULL;
+        if (g.dim == 1) group = 0;
+        if (g.cols != D || (g.dim == 2 && g.rows != (int)(((long long)M + group - 1) / group)))
+            return refuse("gate", "the shape does not fit the other operands"), NULL;
+    }
+    const double scale = PyFloat_AsDouble(a[6]);
+    if (PyErr_Occurred()) return NULL;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_residual_norm(r.ptr, r.ld, r.ptr ? r.kind : h.kind, y.ptr, y.ld, y.kind, &post, g.ptr, g.ld, g.kind, group, (float)scale, &pre, M, D,
+                         h.ptr, h.ld, x.ptr, x.ld, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* bind(muxq_linear, muxq_linear_bias, muxq_quantize, get_device, raw_stream, float16, float32[, muxq_residual_norm]) */
 static PyObject *bind(PyObject *self, PyObject *const *a, Py_ssize_t n) {
-    if (n != 7) return PyErr_Format(PyExc_TypeError, "bind takes 7 arguments");
+    if (n != 7 && n != 8) return PyErr_Format(PyExc_TypeError, "bind takes 7 or 8 arguments");
     f_linear = (linear_fn)PyLong_AsVoidPtr(a[0]);
     f_linear_bias = (linear_bias_fn)PyLong_AsVoidPtr(a[1]);
     f_quantize = (quantize_fn)PyLong_AsVoidPtr(a[2]);
+    if (n > 7) f_residual_norm = (residual_norm_fn)PyLong_AsVoidPtr(a[7]);
     if (PyErr_Occurred()) return NULL;
     Py_XSETREF(get_device, Py_NewRef(a[3]));
     Py_XSETREF(raw_stream, Py_NewRef(a[4]));
@@ -200,6 +301,7 @@ static PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, "addresses of the entry points, torch's stream lookup and dtypes"},
     {"linear", (PyCFunction)(void (*)(void))linear, METH_FASTCALL, "muxq_linear / muxq_linear_bias"},
     {"quantize_weight", (PyCFunction)(void (*)(void))quantize_weight, METH_FASTCALL, "muxq_quantize(is_weight = 1)"},
+    {"residual_norm", (PyCFunction)(void (*)(void))residual_norm, METH_FASTCALL, "muxq_residual_norm"},
     {"stream", stream, METH_NOARGS, "handle of the current stream"},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
@@ -207,7 +309,7 @@ static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, m
 PyMODINIT_FUNC PyInit__calls(void) {
     struct { PyObject **to; const char *name; } names[] = {
         {&n_data_ptr, "data_ptr"}, {&n_shape, "shape"}, {&n_stride, "stride"}, {&n_dtype, "dtype"}, {&n_is_cuda, "is_cuda"},
-        {&n_numel, "numel"}, {&n_is_contiguous, "is_contiguous"}, {&n_threshold, "threshold"}, {&n_exp_factor, "exp_factor"}, {&n_act_bits, "act_bits"},
+        {&n_numel, "numel"}, {&n_is_contiguous, "is_contiguous"}, {&n_get_device, "get_device"}, {&n_threshold, "threshold"}, {&n_exp_factor, "exp_factor"}, {&n_act_bits, "act_bits"},
         {&n_w_bits, "w_bits"}, {&n_gran, "gran"}, {&n_aux_scale, "aux_scale"}, {&n_max_outliers, "max_outliers"}};
     for (size_t i = 0; i < sizeof names / sizeof *names; ++i)
         if (!*names[i].to && !(*names[i].to = PyUnicode_InternFromString(names[i].name))) return NULL;
