@@ -349,6 +349,36 @@ int muxq_residual_norm(const void *R, int ldr, int res_kind, const void *Y, int 
                        const void *gate, int ldg, int gate_kind, int gate_group, float alpha, const muxq_norm *pre, int M,
                        int D, void *H, int ldh, void *X_f16, int ldx, void *stream);
 
+/*
+ * Low-rank adapters of many requests beside a shared projection (the paper quantizes the projection; the adapters stay as they are):
+ *   Y[m, :] = base[m, :] + scale[a] * (X[m, :] A[a]^T) B[a]^T,   a = row_slot[m]
+ * for a batch whose token rows belong to different adapters, in any order; row_slot[m] = -1: no adapter, Y[m] = base[m].  The products
+ * of fp16 values are summed in fp32, X A^T keeps 22 bits of its value on the way into the second product, the sum with base is rounded once.
+ *   X     [M, ldx] fp16;  base, Y  [M, ldbase], [M, ldy] by out_kind (MUXQ_OUT_F16 / MUXQ_OUT_F32); base NULL: 0; base may be Y
+ *         itself (same address and pitch): a projection's result, added to in place
+ *   A     [slots][max_rank, lda >= K] fp16, stride_a elements from slot to slot;   B  [slots][N, ldb >= max_rank] fp16, stride_b
+ *   rank  device int32 [slots], 0 <= rank <= max_rank, or NULL: max_rank everywhere.  Rows of A[a] and columns of B[a] from rank[a]
+ *         on are not used, whatever they hold; rank 0 is a slot without an adapter
+ *   scale device fp32 [slots], or NULL: 1
+ *   row_slot  device int32 [M]
+ *   dev_status  device int32 (sticky): raised to MUXQ_ERR_INVALID_ARG when a used row_slot or rank is out of range; the rows
+ *         concerned are then taken as rows without an adapter
+ * Everything is read in stream order (an adapter may be loaded into a slot by work ahead of the call).  Y overlaps nothing but base;
+ * rows behind M and columns behind N are left as they are.  Results do not depend on the other rows of the batch but for the order
+ * of the sums over K, and are the same from call to call.  K, N, max_rank, pitches and strides are multiples of 8 (pitch of
+ * an fp32 matrix: 4), max_rank <= 128, X, A, B, base and Y 16-byte aligned.  No workspace.
+ */
+typedef struct muxq_adapter_set {
+    const void *A_f16, *B_f16;
+    int lda, ldb;
+    int64_t stride_a, stride_b;
+    const float *scale;  /* or NULL */
+    const int32_t *rank; /* or NULL */
+    int slots, max_rank;
+} muxq_adapter_set;
+int muxq_adapters(const void *X_f16, int M, int K, int ldx, const muxq_adapter_set *set, const int32_t *row_slot, int N,
+                  const void *base, int ldbase, void *Y, int ldy, int out_kind, int32_t *dev_status, void *stream);
+
 /* Synchronizes `stream` and returns the device status word (or MUXQ_ERR_CUDA). */
 int muxq_read_status(const int32_t *dev_status, void *stream);
 

@@ -25,7 +25,7 @@ EXPORTS = (
     "muxq_host_workspace_bytes", "muxq_workspace_init", "muxq_workspace_view", "muxq_detect_outliers", "muxq_build_aux",
     "muxq_quantize", "muxq_gemm", "muxq_linear", "muxq_linear_bias", "muxq_linear_events", "muxq_linear_host",
     "muxq_linear_decode_noalloc", "muxq_int8_mma_peak", "muxq_test_hooks", "muxq_test_late_warps", "muxq_read_status",
-    "muxq_residual_norm", "muxq_chain_plan_bytes", "muxq_chain_device_bytes", "muxq_chain_build", "muxq_chain_run",
+    "muxq_residual_norm", "muxq_adapters", "muxq_chain_plan_bytes", "muxq_chain_device_bytes", "muxq_chain_build", "muxq_chain_run",
     "muxq_status_string",
 )
 
@@ -103,6 +103,7 @@ def lib() -> ctypes.CDLL:
         L.muxq_test_hooks.argtypes = [vp]; L.muxq_test_hooks.restype = i
         L.muxq_test_late_warps.argtypes = [ctypes.c_uint32]; L.muxq_test_late_warps.restype = i
         L.muxq_residual_norm.argtypes = [vp, i, i, vp, i, i, vp, vp, i, i, i, f, vp, i, i, vp, i, vp, i, vp]; L.muxq_residual_norm.restype = i
+        L.muxq_adapters.argtypes = [vp, i, i, i, vp, vp, i, vp, i, vp, i, i, vp, vp]; L.muxq_adapters.restype = i
         L.muxq_chain_plan_bytes.argtypes = [i]; L.muxq_chain_plan_bytes.restype = sz
         L.muxq_chain_device_bytes.argtypes = [vp, i, i]; L.muxq_chain_device_bytes.restype = sz
         L.muxq_chain_build.argtypes = [vp, i, i, pp, i, vp, sz, vp, sz, vp]; L.muxq_chain_build.restype = i
@@ -112,7 +113,8 @@ def lib() -> ctypes.CDLL:
         from . import _calls as calls
         at = lambda entry: ctypes.cast(entry, vp).value
         calls.bind(at(L.muxq_linear), at(L.muxq_linear_bias), at(L.muxq_quantize), torch._C._cuda_getDevice,
-                   torch._C._cuda_getCurrentRawStream, torch.float16, torch.float32, at(L.muxq_residual_norm))
+                   torch._C._cuda_getCurrentRawStream, torch.float16, torch.float32, at(L.muxq_residual_norm),
+                   at(L.muxq_adapters), torch.int32)
         _calls = calls  # first: a thread that finds _lib set goes on to use it
         _lib = L
     return _lib
@@ -262,13 +264,47 @@ def muxq_gemm(body_q: torch.Tensor, aux_q: Optional[torch.Tensor], w_q: torch.Te
 
 def muxq_linear(X: torch.Tensor, w_q: torch.Tensor, s_w: torch.Tensor, p: MuxqParams, ws: Workspace,
                 out_kind: int = MUXQ_OUT_F16, out: Optional[torch.Tensor] = None,
-                bias: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Y = MUXQ-quantized X.W [+ bias]; w_q [N,K] int8 and s_w from muxq_quantize(is_weight=True); bias fp32 [N]."""
+                bias: Optional[torch.Tensor] = None, adapters: Optional["Adapters"] = None) -> torch.Tensor:
+    """Y = MUXQ-quantized X.W [+ bias] [+ the adapters of the rows' requests]; w_q [N,K] int8 and s_w from
+    muxq_quantize(is_weight=True); bias fp32 [N].  The adapters are a call of muxq_adapters behind the layer, added to Y in place
+    (an fp16 Y is rounded before and behind them)."""
     Y = out if out is not None else _alloc_out(X.shape[0], w_q.shape[0], out_kind, X.device)
+    if adapters is not None and out_kind == MUXQ_OUT_ACC_I32:
+        raise MuxqError("muxq_adapters", MUXQ_ERR_INVALID_ARG)  # they belong to the dequantized output
     rc = _hot().linear(X, w_q, s_w, p, ws.buf, ws.status, out_kind, Y, bias)
     if rc:
         raise MuxqError("muxq_linear" if bias is None else "muxq_linear_bias", rc)
+    if adapters is not None:
+        muxq_adapters(X, adapters.A, adapters.B, adapters.row_slot, ws.status, adapters.scale, adapters.rank, base=Y, out=Y)
     return Y
+
+
+class Adapters(NamedTuple):
+    """What muxq_adapters takes beside X: A [slots, R, K] and B [slots, N, R] fp16, row_slot int32 [M] (-1: none), scale fp32 [slots]
+    and rank int32 [slots] or None."""
+    A: torch.Tensor
+    B: torch.Tensor
+    row_slot: torch.Tensor
+    scale: Optional[torch.Tensor] = None
+    rank: Optional[torch.Tensor] = None
+
+
+def muxq_adapters(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, row_slot: torch.Tensor, status: torch.Tensor,
+                  scale: Optional[torch.Tensor] = None, rank: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None,
+                  out_kind: Optional[int] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Y[m] = base[m] + scale[a] * (X[m] A[a]^T) B[a]^T with a = row_slot[m] (-1: no adapter): the low-rank adapters of a batch's
+    requests beside the projection they share.  A [slots, R, K] and B [slots, N, R] fp16, rank int32 [slots] (None: R everywhere;
+    what lies beyond a slot's rank is not used), scale fp32 [slots] (None: 1).  base is the projection's result, fp16 or fp32 (None: 0), and may
+    be `out`.  Y has the type of base, or out_kind.  status: device int32[1], raised on a slot or a rank out of range."""
+    if out is None:
+        kind = out_kind if out_kind is not None else MUXQ_OUT_F32 if base is not None and base.dtype == torch.float32 else MUXQ_OUT_F16
+        if kind == MUXQ_OUT_ACC_I32:
+            raise MuxqError("muxq_adapters", MUXQ_ERR_INVALID_ARG)
+        out = _alloc_out(X.shape[0], B.shape[1], kind, X.device)
+    rc = _hot().adapters(X, A, B, row_slot, scale, rank, base, out, status)
+    if rc:
+        raise MuxqError("muxq_adapters", rc)
+    return out
 
 
 def muxq_linear_events(X: torch.Tensor, w_q: torch.Tensor, s_w: torch.Tensor, p: MuxqParams, ws: Workspace,

@@ -597,6 +597,42 @@ int muxq_residual_norm(const void *R, int ldr, int res_kind, const void *Y, int 
     return cuda_rc(launch_residual_norm(a, static_cast<cudaStream_t>(stream)));
 }
 
+int muxq_adapters(const void *X, int M, int K, int ldx, const muxq_adapter_set *set, const int32_t *row_slot, int N,
+                  const void *base, int ldbase, void *Y, int ldy, int out_kind, int32_t *dev_status, void *stream) {
+    if (!X || !set || !set->A_f16 || !set->B_f16 || !row_slot || !Y || !dev_status || M <= 0 || K <= 0 || N <= 0 || set->slots <= 0 ||
+        set->max_rank <= 0 || ldx < K || set->lda < K || set->ldb < set->max_rank || ldy < N || (base && ldbase < N) || !real_kind(out_kind) ||
+        (set->slots > 1 && (set->stride_a < (int64_t)(set->max_rank - 1) * set->lda + K || set->stride_b < (int64_t)(N - 1) * set->ldb + set->max_rank)))
+        return MUXQ_ERR_INVALID_ARG;
+    if (K % 8 || N % 8 || set->max_rank % 8 || set->max_rank > kAdapterMaxRank || ldx % 8 || set->lda % 8 || set->ldb % 8 ||
+        (set->slots > 1 && (set->stride_a % 8 || set->stride_b % 8)) || !pitch_ok(ldy, out_kind) || (base && !pitch_ok(ldbase, out_kind)) || !aligned16(X) ||
+        !aligned16(set->A_f16) || !aligned16(set->B_f16) || !aligned16(Y) || !aligned16(base))
+        return MUXQ_ERR_UNSUPPORTED;
+    const Span x = span(X, M, K, ldx, MUXQ_OUT_F16), b = span(base, M, N, ldbase, out_kind), y = span(Y, M, N, ldy, out_kind);
+    const size_t last = (size_t)(set->slots - 1);
+    const Span wa{set->A_f16, 1, 1, ((last ? last * set->stride_a : 0) + (size_t)(set->max_rank - 1) * set->lda + K) * 2};
+    const Span wb{set->B_f16, 1, 1, ((last ? last * set->stride_b : 0) + (size_t)(N - 1) * set->ldb + set->max_rank) * 2};
+    const Span ids{row_slot, 1, 1, (size_t)M * 4}, sc{set->scale, 1, 1, (size_t)set->slots * 4}, rk{set->rank, 1, 1, (size_t)set->slots * 4};
+    if ((overlap(y, b) && !same_place(y, b)) || overlap(y, x) || overlap(y, wa) || overlap(y, wb) || overlap(y, ids) || overlap(y, sc) ||
+        overlap(y, rk))
+        return MUXQ_ERR_INVALID_ARG;
+    AdapterArgs a{};
+    a.X = static_cast<const __half *>(X);
+    a.M = M; a.K = K; a.ldx = ldx;
+    a.A = static_cast<const __half *>(set->A_f16);
+    a.B = static_cast<const __half *>(set->B_f16);
+    a.lda = set->lda; a.ldb = set->ldb;
+    a.stride_a = set->slots > 1 ? set->stride_a : 0;
+    a.stride_b = set->slots > 1 ? set->stride_b : 0;
+    a.scale = set->scale; a.rank = set->rank;
+    a.slots = set->slots; a.max_rank = set->max_rank;
+    a.row_slot = row_slot;
+    a.N = N;
+    a.base = base; a.ldbase = ldbase;
+    a.Y = Y; a.ldy = ldy; a.out_f32 = out_kind == MUXQ_OUT_F32;
+    a.dev_status = dev_status;
+    return cuda_rc(launch_adapters(a, static_cast<cudaStream_t>(stream)));
+}
+
 // ---------------------------------------------------------------- lists of decode-shaped layers
 // A list in which some layer reads what the one before it wrote runs as one persistent launch that hands layers on
 // (k4s_decode_stream.cu); a list of independent layers as a preparation and a weight stream (k4t_decode_list.cu).

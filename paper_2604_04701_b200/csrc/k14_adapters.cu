@@ -1,0 +1,347 @@
+// Low-rank adapters of many requests beside a shared projection:
+//   Y[m] = base[m] + s_a * (X[m] A_a^T) B_a^T,   a = slot[m]
+// in one launch.  A cluster of CTAs takes a window of consecutive token rows.  It sorts them by adapter, so that rows of one adapter
+// share m16 tiles of matrix instructions wherever in the window they stand; its CTAs divide K between them for T = X A^T, exchange
+// their parts of T through distributed shared memory, and divide N for T B^T.
+//
+// T is held in fp32.  For the second product every row of T is scaled by a power of two (exact; undone in fp32 afterwards) and split into two
+// fp16 numbers whose sum has 22 bits of it: one fp16 number alone would put an error of 2^-11 on an fp32 result, and rows
+// of large activations would leave its range.
+//
+// The matrix instructions are the ones that read registers (m16n8k16): at ranks up to 64 the operator is bound by X, base and Y in HBM,
+// and operands whose order of k may be chosen freely go from global memory to registers in whole 16-byte words without a
+// detour; n is permuted so that a thread ends up with eight neighbouring results.
+#include <limits.h>
+
+#include "../../include/muxq.h"
+#include "kernels.h"
+#include "ptx.cuh"
+
+namespace muxq {
+
+namespace {
+
+constexpr int kT = 256, kWarps = kT / 32;
+constexpr int kMostRows = 64;  // of a window
+
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// Rows of T parts (fp32) and of T itself (per four ranks: four upper halves, four lower halves); the pitches keep the eight rows of
+// a fragment on different banks.
+template <int NR> __host__ __device__ constexpr int part_pitch() { return NR * 8 + 8; }                              // floats
+template <int NR> __host__ __device__ constexpr int t_pitch() { return (NR * 32 / 64 | 1) * 64; }                    // bytes
+template <int NR> __host__ __device__ constexpr size_t smem_bytes(int W) {
+    const int rows = W * kWarps < 128 ? W * kWarps : 128;  // (see k_adapters: slices of K times rows)
+    return (size_t)rows * part_pitch<NR>() * 4 + (size_t)W * t_pitch<NR>();
+}
+
+// eight neighbouring results
+__device__ __forceinline__ void add_store(__half *y, const uint4 &b, const float (&v)[8], float f) {
+    const __half2 *h = reinterpret_cast<const __half2 *>(&b);
+    uint4 o;
+    __half2 *q = reinterpret_cast<__half2 *>(&o);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 c = __half22float2(h[i]);
+        q[i] = __floats2half2_rn(__fmaf_rn(f, v[2 * i], c.x), __fmaf_rn(f, v[2 * i + 1], c.y));
+    }
+    *reinterpret_cast<uint4 *>(y) = o;
+}
+struct Eight32 { float4 a, b; };
+__device__ __forceinline__ void add_store(float *y, const Eight32 &b, const float (&v)[8], float f) {
+    float4 *o = reinterpret_cast<float4 *>(y);
+    o[0] = make_float4(__fmaf_rn(f, v[0], b.a.x), __fmaf_rn(f, v[1], b.a.y), __fmaf_rn(f, v[2], b.a.z), __fmaf_rn(f, v[3], b.a.w));
+    o[1] = make_float4(__fmaf_rn(f, v[4], b.b.x), __fmaf_rn(f, v[5], b.b.y), __fmaf_rn(f, v[6], b.b.z), __fmaf_rn(f, v[7], b.b.w));
+}
+template <typename T> struct EightOf;
+template <> struct EightOf<__half> { using type = uint4; };
+template <> struct EightOf<float> { using type = Eight32; };
+
+struct Tiles {  // a window's rows in order of their adapters
+    int row[kMostRows];      // by position: row within the window
+    int slot[kMostRows];     // by position; rows without an adapter come last
+    float factor[kMostRows]; // by position: what T B^T is multiplied by
+    int rank_of[kMostRows];  // by position
+    int key[kMostRows];      // by row: its adapter, INT_MAX without one
+    bool start[kMostRows];   // by row: the first of a tile
+    int pos[kMostRows], count[kMostRows], rank[kMostRows];  // by tile: first position, rows (up to 16), rank
+};
+
+template <int NR, typename TO>
+__global__ void __launch_bounds__(kT, 2) k_adapters(const AdapterArgs a, int W, int C) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ Tiles s;
+    constexpr int kPP = part_pitch<NR>(), kTP = t_pitch<NR>();
+    using Eight = typename EightOf<TO>::type;
+    float *part = reinterpret_cast<float *>(smem);
+    uint8_t *tsm = smem + smem_bytes<NR>(W) - (size_t)W * kTP;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int cta = C > 1 ? (int)cluster_ctarank() : 0;
+    const int m0 = (int)(blockIdx.x / C) * W, rows = min(W, a.M - m0);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // behind the wait: a layer kernel may read its W_q at once
+
+    // ---- rows in order of their adapters, and tiles of up to 16 rows of one adapter
+    int key = INT_MAX, rank = 0;
+    if (tid < rows) {
+        const int slot = a.row_slot[m0 + tid];
+        bool bad = slot < -1 || slot >= a.slots;
+        if (!bad && slot >= 0) {
+            rank = a.rank ? a.rank[slot] : a.max_rank;
+            bad = rank < 0 || rank > a.max_rank;
+            if (!bad && rank > 0) key = slot;
+        }
+        if (bad) {
+            rank = 0;
+            if (cta == 0) atomicMax(a.dev_status, MUXQ_ERR_INVALID_ARG);
+        }
+        s.key[tid] = key;
+    }
+    const int active = __syncthreads_count(key != INT_MAX);
+    int at = 0, same = 0, of_key = 0;
+    if (tid < rows) {
+        int before = 0;
+        for (int j = 0; j < rows; ++j) {
+            const int k = s.key[j];
+            before += k < key;
+            same += k == key && j < tid;
+            of_key += k == key;
+        }
+        at = before + same;
+        s.row[at] = tid;
+        s.slot[at] = key == INT_MAX ? -1 : key;
+        s.rank_of[at] = rank;
+    }
+    const bool start = key != INT_MAX && same % 16 == 0;
+    if (tid < rows) s.start[tid] = start;
+    const int tiles = __syncthreads_count(start);
+    if (start) {
+        int i = same / 16;
+        for (int j = 0; j < rows; ++j) i += s.start[j] && s.key[j] < key;
+        s.pos[i] = at;
+        s.count[i] = min(16, of_key - same);
+        s.rank[i] = rank;
+    }
+    __syncthreads();
+
+    // ---- T = X A^T: this CTA's part of K.  With fewer tiles than warps the warps divide it further.
+    int lanes_t = 1;  // warps side by side on different tiles: tiles rounded up to a power of two, at most all
+    while (lanes_t < kWarps && lanes_t < tiles) lanes_t *= 2;
+    const int slices = kWarps / lanes_t, wt = warp & (lanes_t - 1), wk = warp / lanes_t;
+    {
+        const int chunks = (a.K + 31) >> 5, c0 = (int)((long long)chunks * cta / C), c1 = (int)((long long)chunks * (cta + 1) / C);
+        for (int i = wt; i < tiles; i += lanes_t) {
+            const int p0 = s.pos[i], n = s.count[i], r = s.rank[i];
+            float acc[NR][4];
+#pragma unroll
+            for (int j = 0; j < NR; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
+            const bool in0 = g < n, in1 = g + 8 < n;
+            const __half *x0 = a.X + (size_t)(m0 + s.row[in0 ? p0 + g : p0]) * a.ldx + 8 * t;
+            const __half *x1 = a.X + (size_t)(m0 + s.row[in1 ? p0 + g + 8 : p0]) * a.ldx + 8 * t;
+            const __half *A = a.A + (size_t)s.slot[p0] * a.stride_a + (size_t)g * a.lda + 8 * t;
+            const uint4 z = make_uint4(0, 0, 0, 0);
+#pragma unroll 2
+            for (int c = c0 + wk; c < c1; c += slices) {
+                const bool in = c * 32 + 8 * t < a.K;
+                const uint4 u = in && in0 ? *reinterpret_cast<const uint4 *>(x0 + c * 32) : z;
+                const uint4 v = in && in1 ? *reinterpret_cast<const uint4 *>(x1 + c * 32) : z;
+#pragma unroll
+                for (int j = 0; j < NR; ++j) {
+                    if (j * 8 < r) {
+                        const uint4 w = in && j * 8 + g < r ? *reinterpret_cast<const uint4 *>(A + (size_t)j * 8 * a.lda + c * 32) : z;
+                        mma16816(acc[j], u.x, v.x, u.y, v.y, w.x, w.y);
+                        mma16816(acc[j], u.z, v.z, u.w, v.w, w.z, w.w);
+                    }
+                }
+            }
+            float *to = part + (size_t)(wk * active + p0) * kPP + 2 * t;
+#pragma unroll
+            for (int j = 0; j < NR; ++j) {
+                if (j * 8 < r) {
+                    if (in0) *reinterpret_cast<float2 *>(to + g * kPP + j * 8) = make_float2(acc[j][0], acc[j][1]);
+                    if (in1) *reinterpret_cast<float2 *>(to + (g + 8) * kPP + j * 8) = make_float2(acc[j][2], acc[j][3]);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    if (slices > 1) {
+        for (int i = tid; i < active * NR * 8; i += kT) {
+            const int p = i / (NR * 8), r = i - p * (NR * 8);
+            if (r < s.rank_of[p]) {
+                float v = part[p * kPP + r];
+                for (int k = 1; k < slices; ++k) v += part[(k * active + p) * kPP + r];
+                part[p * kPP + r] = v;
+            }
+        }
+        if (C == 1) __syncthreads();
+    }
+    if (C > 1) cluster_sync_all();
+
+    // ---- the whole of T: parts of the other CTAs, scaled and split
+    for (int p = warp; p < active; p += kWarps) {
+        constexpr int kPer = (NR * 8 + 31) / 32;
+        const int r = s.rank_of[p];
+        float v[kPer], most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int j = lane + 32 * i;
+            v[i] = 0.0f;
+            if (j < r) {
+                if (C == 1) {
+                    v[i] = part[p * kPP + j];
+                } else {
+                    const uint32_t from = smem_u32(part + p * kPP + j);
+                    for (int c = 0; c < C; ++c) v[i] += ld_cluster_f32(map_to_cta(from, c));
+                }
+            }
+            most = fmaxf(most, fabsf(v[i]));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        // the largest of the row lands in [2^13, 2^14); a row of nothing but tiny values stays below
+        int e = 13 - ((int)(__float_as_uint(most) >> 23) - 127);
+        if (e > 100 || most == 0.0f) e = most == 0.0f ? 0 : 100;
+        const float up = __uint_as_float((uint32_t)(127 + e) << 23), down = __uint_as_float((uint32_t)(127 - e) << 23);
+        uint8_t *to = tsm + p * kTP;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int j = lane + 32 * i;
+            if (j < NR * 8) {
+                const float x = v[i] * up;
+                const __half hi = __float2half_rn(x), lo = __float2half_rn(x - __half2float(hi));
+                *reinterpret_cast<__half *>(to + (j >> 2) * 16 + (j & 3) * 2) = hi;
+                *reinterpret_cast<__half *>(to + (j >> 2) * 16 + 8 + (j & 3) * 2) = lo;
+            }
+        }
+        if (lane == 0) s.factor[p] = (a.scale ? a.scale[s.slot[p]] : 1.0f) * down;
+    }
+    __syncthreads();
+    // every CTA has read the others' parts behind this point: waited for at the end
+    if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+
+    // ---- Y = base + T B^T: this CTA's part of N
+    const int chunks = (a.N + 31) >> 5, q0 = (int)((long long)chunks * cta / C), q1 = (int)((long long)chunks * (cta + 1) / C);
+    const TO *base = static_cast<const TO *>(a.base);
+    TO *Y = static_cast<TO *>(a.Y);
+    const Eight none{};
+    for (int q = q0 + warp; q < q1; q += kWarps) {
+        const int n0 = q * 32 + 8 * t;
+        const bool in = n0 < a.N;
+        for (int i = 0; i < tiles; ++i) {
+            const int p0 = s.pos[i], n = s.count[i], r = s.rank[i];
+            const bool in0 = in && g < n, in1 = in && g + 8 < n;
+            const size_t r0 = m0 + s.row[in0 ? p0 + g : p0], r1 = m0 + s.row[in1 ? p0 + g + 8 : p0];
+            const Eight b0 = in0 && base ? *reinterpret_cast<const Eight *>(base + r0 * a.ldbase + n0) : none;
+            const Eight b1 = in1 && base ? *reinterpret_cast<const Eight *>(base + r1 * a.ldbase + n0) : none;
+            float acc[4][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
+            const __half *B = a.B + (size_t)s.slot[p0] * a.stride_b + 4 * t;
+            const uint8_t *t0 = tsm + (p0 + (g < n ? g : 0)) * kTP + t * 16, *t1 = tsm + (p0 + (g + 8 < n ? g + 8 : 0)) * kTP + t * 16;
+#pragma unroll
+            for (int k = 0; k < NR / 2; ++k) {
+                if (k * 16 < r) {
+                    const uint4 u = *reinterpret_cast<const uint4 *>(t0 + k * 64), v = *reinterpret_cast<const uint4 *>(t1 + k * 64);
+                    const int k0 = k * 16 + 4 * t;  // this lane's four ranks
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int col = q * 32 + (g >> 1) * 8 + 2 * j + (g & 1);
+                        uint2 w = col < a.N && k0 < r ? *reinterpret_cast<const uint2 *>(B + (size_t)col * a.ldb + k * 16) : make_uint2(0, 0);
+                        if (k0 + 4 > r) {  // ranks beyond this adapter's own are not looked at
+                            if (k0 + 1 >= r) w.x &= 0xffffu;
+                            if (k0 + 2 >= r) w.y = 0;
+                            if (k0 + 3 >= r) w.y &= 0xffffu;
+                        }
+                        mma16816(acc[j], u.x, v.x, u.y, v.y, w.x, w.y);
+                        mma16816(acc[j], u.z, v.z, u.w, v.w, w.x, w.y);
+                    }
+                }
+            }
+            const float f0 = s.factor[p0 + (g < n ? g : 0)], f1 = s.factor[p0 + (g + 8 < n ? g + 8 : 0)];
+            const float o0[8] = {acc[0][0], acc[0][1], acc[1][0], acc[1][1], acc[2][0], acc[2][1], acc[3][0], acc[3][1]};
+            const float o1[8] = {acc[0][2], acc[0][3], acc[1][2], acc[1][3], acc[2][2], acc[2][3], acc[3][2], acc[3][3]};
+            if (in0) add_store(Y + r0 * a.ldy + n0, b0, o0, f0);
+            if (in1) add_store(Y + r1 * a.ldy + n0, b1, o1, f1);
+        }
+    }
+    // ---- rows without an adapter
+    if (base != Y) {
+        const int first = q0 * 4, last = min(q1 * 4, a.N >> 3);  // in eights of columns
+        for (int p = active + warp; p < rows; p += kWarps) {
+            const size_t r = m0 + s.row[p];
+            for (int c = first + lane; c < last; c += 32)
+                *reinterpret_cast<Eight *>(Y + r * a.ldy + c * 8) = base ? *reinterpret_cast<const Eight *>(base + r * a.ldbase + c * 8) : none;
+        }
+    }
+    __syncwarp();
+    if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+template <int NR, typename TO>
+cudaError_t launch_form(const AdapterArgs &a, int W, int C, cudaStream_t s) {
+    static PerDevice<int> done;
+    const int dev = current_device();
+    if (dev < 0) return cudaErrorInvalidDevice;
+    {
+        std::lock_guard<std::mutex> lock(device_mutex());
+        if (!done.have[dev]) {
+            const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(k_adapters<NR, TO>), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                       (int)smem_bytes<NR>(kMostRows));
+            if (e != cudaSuccess) return e;
+            done.have[dev] = true;
+        }
+    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)((((long long)a.M + W - 1) / W) * C));
+    cfg.blockDim = dim3(kT);
+    cfg.dynamicSmemBytes = smem_bytes<NR>(W);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = C; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = C > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, k_adapters<NR, TO>, a, W, C);
+}
+
+template <typename TO>
+cudaError_t launch_type(const AdapterArgs &a, int W, int C, cudaStream_t s) {
+    if (a.max_rank <= 16) return launch_form<2, TO>(a, W, C, s);
+    if (a.max_rank <= 32) return launch_form<4, TO>(a, W, C, s);
+    if (a.max_rank <= 64) return launch_form<8, TO>(a, W, C, s);
+    return launch_form<16, TO>(a, W, C, s);
+}
+
+// Rows of a window and CTAs of its cluster.
+void choose(const AdapterArgs &a, int sms, int *W, int *C) {
+    int w = 1;
+    while (w < kMostRows && ((long long)a.M + w - 1) / w * 8 > 2 * sms) w *= 2;
+    int c = 8;
+    while (c > 1 && ((long long)a.M + w - 1) / w * c > 2 * sms) c /= 2;
+    *W = w;
+    *C = c;
+}
+
+}  // namespace
+
+cudaError_t launch_adapters(const AdapterArgs &a, cudaStream_t s) {
+    const int sms = num_sms();
+    if (sms < 1) return cudaErrorInvalidDevice;
+    int W, C;
+    choose(a, sms, &W, &C);
+    return a.out_f32 ? launch_type<float>(a, W, C, s) : launch_type<__half>(a, W, C, s);
+}
+
+}  // namespace muxq

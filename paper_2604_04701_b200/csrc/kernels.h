@@ -320,6 +320,27 @@ struct ResidualNormArgs {
 constexpr int kNormMaxD = 16384;
 cudaError_t launch_residual_norm(const ResidualNormArgs &a, cudaStream_t s);
 
+// Y[m] = base[m] + scale[a] * (X[m] A[a]^T) B[a]^T, a = row_slot[m] (k14_adapters.cu)
+constexpr int kAdapterMaxRank = 128;
+struct AdapterArgs {
+    const __half *X;
+    int M, K, ldx;
+    const __half *A, *B;        // [slots][max_rank, lda], [slots][N, ldb]
+    int lda, ldb;
+    int64_t stride_a, stride_b; // elements from slot to slot
+    const float *scale;         // [slots] or NULL: 1
+    const int32_t *rank;        // [slots] or NULL: max_rank
+    int slots, max_rank;
+    const int32_t *row_slot;    // [M], -1: none
+    int N;
+    const void *base;           // type of Y; NULL: zero; may be Y
+    int ldbase;
+    void *Y;
+    int ldy, out_f32;
+    int32_t *dev_status;        // raised on a slot or a rank out of range
+};
+cudaError_t launch_adapters(const AdapterArgs &a, cudaStream_t s);
+
 cudaError_t launch_mma_peak(int n, int iters, unsigned long long *cycles_out, int32_t *status, int grid,
                             cudaStream_t s);
 

@@ -21,11 +21,15 @@ typedef int (*quantize_fn)(const void *, int, int, int, const muxq_params *, int
 typedef int (*residual_norm_fn)(const void *, int, int, const void *, int, int, const muxq_norm *, const void *, int, int, int, float,
                                 const muxq_norm *, int, int, void *, int, void *, int, void *);
 
+typedef int (*adapters_fn)(const void *, int, int, int, const muxq_adapter_set *, const int32_t *, int, const void *, int, void *, int, int,
+                           int32_t *, void *);
+
 static linear_fn f_linear;
 static linear_bias_fn f_linear_bias;
 static quantize_fn f_quantize;
 static residual_norm_fn f_residual_norm;
-static PyObject *get_device, *raw_stream, *dt_f16, *dt_f32;
+static adapters_fn f_adapters;
+static PyObject *get_device, *raw_stream, *dt_f16, *dt_f32, *dt_i32;
 static PyObject *n_data_ptr, *n_shape, *n_stride, *n_dtype, *n_is_cuda, *n_numel, *n_is_contiguous, *n_get_device;
 static PyObject *n_threshold, *n_exp_factor, *n_act_bits, *n_w_bits, *n_gran, *n_aux_scale, *n_max_outliers;
 
@@ -282,18 +286,88 @@ static PyObject *residual_norm(PyObject *self, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(rc);
 }
 
-/* bind(muxq_linear, muxq_linear_bias, muxq_quantize, get_device, raw_stream, float16, float32[, muxq_residual_norm]) */
+/* a 3-D fp16 tensor: [n][rows, cols] */
+static int stack_of(PyObject *t, const char *what, int device, void **ptr, int *n, int *rows, int *cols, int *ld, int64_t *stride) {
+    int at = -1, f16;
+    if (as_int(PyObject_CallMethodNoArgs(t, n_get_device), &at)) return -1;
+    if (at < 0) return refuse(what, "a CUDA tensor is wanted");
+    if (at != device) return refuse(what, "the tensor is on another device than the current one");
+    if ((f16 = has_dtype(t, dt_f16)) < 0) return -1;
+    if (!f16) return refuse(what, "fp16 is wanted");
+    PyObject *shape = PyObject_GetAttr(t, n_shape), *st = shape ? PyObject_CallMethodNoArgs(t, n_stride) : NULL;
+    int rc = shape && st ? 0 : -1, last = 1;
+    if (!rc && (!PyTuple_Check(shape) || PyTuple_GET_SIZE(shape) != 3 || !PyTuple_Check(st) || PyTuple_GET_SIZE(st) != 3))
+        rc = refuse(what, "three dimensions are wanted");
+    if (!rc) {
+        rc = as_int(Py_NewRef(PyTuple_GET_ITEM(shape, 0)), n) || as_int(Py_NewRef(PyTuple_GET_ITEM(shape, 1)), rows) ||
+                     as_int(Py_NewRef(PyTuple_GET_ITEM(shape, 2)), cols) || as_int(Py_NewRef(PyTuple_GET_ITEM(st, 1)), ld) ||
+                     as_int(Py_NewRef(PyTuple_GET_ITEM(st, 2)), &last)
+                 ? -1
+                 : 0;
+        *stride = PyLong_AsLongLong(PyTuple_GET_ITEM(st, 0));
+        if (PyErr_Occurred()) rc = -1;
+        if (!rc && *cols > 1 && last != 1) rc = refuse(what, "unit stride along the last dimension is wanted");
+        if (!rc && *rows == 1) *ld = *cols;
+    }
+    Py_XDECREF(shape);
+    Py_XDECREF(st);
+    return rc ? -1 : tensor_ptr(t, ptr);
+}
+static int vector_i32(PyObject *t, const char *what, int device, int len, const int32_t **out) { /* len < 0: at least one entry */
+    int at = -1, ok, n, second, dim, sa, sb;
+    *out = NULL;
+    if (t == Py_None) return 0;
+    if (as_int(PyObject_CallMethodNoArgs(t, n_get_device), &at)) return -1;
+    if (at != device) return refuse(what, at < 0 ? "a CUDA tensor is wanted" : "the tensor is on another device than the current one");
+    if ((ok = has_dtype(t, dt_i32)) < 0 || shape_of(t, &n, &second, &dim) || stride_of(t, &sa, &sb)) return -1;
+    if (!ok || dim != 1 || (n > 1 && sa != 1) || (len < 0 ? n < 1 : n != len)) return refuse(what, "a contiguous int32 vector is wanted, one entry for each row or slot");
+    return tensor_ptr(t, (void **)out);
+}
+
+/* adapters(X, A, B, row_slot, scale or None, rank or None, base or None, Y, status) -> status code */
+static PyObject *adapters(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "adapters takes 9 arguments");
+    operand x = {0}, b = {0}, y = {0};
+    muxq_adapter_set set = {0};
+    void *s, *pa, *pb;
+    const int32_t *row_slot, *status;
+    int device, K, N, slots, rank;
+    if (current_place(&device, &s) || operand_of(a[0], "X", device, 2, &x) ||
+        stack_of(a[1], "A", device, &pa, &set.slots, &set.max_rank, &K, &set.lda, &set.stride_a) ||
+        stack_of(a[2], "B", device, &pb, &slots, &N, &rank, &set.ldb, &set.stride_b))
+        return NULL;
+    if (x.kind != MUXQ_OUT_F16) return refuse("X", "fp16 is wanted"), NULL;
+    if (x.cols != K) return refuse("A", "the shape does not fit X"), NULL;
+    if (slots != set.slots || rank != set.max_rank) return refuse("B", "the shape does not fit A"), NULL;
+    if (matrix_of(a[7], "Y", device, x.rows, N, &y) || (a[6] != Py_None && matrix_of(a[6], "base", device, x.rows, N, &b)) ||
+        vector_i32(a[3], "row_slot", device, x.rows, &row_slot) || vector_f32(a[4], "scale", device, slots, &set.scale) ||
+        vector_i32(a[5], "rank", device, slots, &set.rank) || vector_i32(a[8], "status", device, -1, &status))
+        return NULL;
+    if (a[6] != Py_None && b.kind != y.kind) return refuse("base", "the type of Y is wanted"), NULL;
+    set.A_f16 = pa;
+    set.B_f16 = pb;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_adapters(x.ptr, x.rows, K, x.ld, &set, row_slot, N, b.ptr, b.ld, y.ptr, y.ld, y.kind, (int32_t *)status, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* bind(muxq_linear, muxq_linear_bias, muxq_quantize, get_device, raw_stream, float16, float32[, muxq_residual_norm[,
+ * muxq_adapters, int32]]) */
 static PyObject *bind(PyObject *self, PyObject *const *a, Py_ssize_t n) {
-    if (n != 7 && n != 8) return PyErr_Format(PyExc_TypeError, "bind takes 7 or 8 arguments");
+    if (n != 7 && n != 8 && n != 10) return PyErr_Format(PyExc_TypeError, "bind takes 7, 8 or 10 arguments");
     f_linear = (linear_fn)PyLong_AsVoidPtr(a[0]);
     f_linear_bias = (linear_bias_fn)PyLong_AsVoidPtr(a[1]);
     f_quantize = (quantize_fn)PyLong_AsVoidPtr(a[2]);
     if (n > 7) f_residual_norm = (residual_norm_fn)PyLong_AsVoidPtr(a[7]);
+    if (n > 8) f_adapters = (adapters_fn)PyLong_AsVoidPtr(a[8]);
     if (PyErr_Occurred()) return NULL;
     Py_XSETREF(get_device, Py_NewRef(a[3]));
     Py_XSETREF(raw_stream, Py_NewRef(a[4]));
     Py_XSETREF(dt_f16, Py_NewRef(a[5]));
     Py_XSETREF(dt_f32, Py_NewRef(a[6]));
+    if (n > 9) Py_XSETREF(dt_i32, Py_NewRef(a[9]));
     Py_RETURN_NONE;
 }
 
@@ -301,6 +375,7 @@ static PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, "addresses of the entry points, torch's stream lookup and dtypes"},
     {"linear", (PyCFunction)(void (*)(void))linear, METH_FASTCALL, "muxq_linear / muxq_linear_bias"},
     {"quantize_weight", (PyCFunction)(void (*)(void))quantize_weight, METH_FASTCALL, "muxq_quantize(is_weight = 1)"},
+    {"adapters", (PyCFunction)(void (*)(void))adapters, METH_FASTCALL, "muxq_adapters"},
     {"residual_norm", (PyCFunction)(void (*)(void))residual_norm, METH_FASTCALL, "muxq_residual_norm"},
     {"stream", stream, METH_NOARGS, "handle of the current stream"},
     {NULL, NULL, 0, NULL}};
