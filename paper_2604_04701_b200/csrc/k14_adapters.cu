@@ -62,6 +62,20 @@ __device__ __forceinline__ void add_store(float *y, const Eight32 &b, const floa
     o[0] = make_float4(__fmaf_rn(f, v[0], b.a.x), __fmaf_rn(f, v[1], b.a.y), __fmaf_rn(f, v[2], b.a.z), __fmaf_rn(f, v[3], b.a.w));
     o[1] = make_float4(__fmaf_rn(f, v[4], b.b.x), __fmaf_rn(f, v[5], b.b.y), __fmaf_rn(f, v[6], b.b.z), __fmaf_rn(f, v[7], b.b.w));
 }
+// ranks of a word from `left` on are set to zero
+__device__ __forceinline__ uint32_t mask_pair(uint32_t v, int left) { return left >= 2 ? v : left == 1 ? v & 0xffffu : 0u; }
+__device__ __forceinline__ void mask_beyond(uint2 &w, int left) {
+    w.x = mask_pair(w.x, left);
+    w.y = mask_pair(w.y, left - 2);
+}
+__device__ __forceinline__ void mask_beyond(uint4 &w, int left) {
+    w.x = mask_pair(w.x, left);
+    w.y = mask_pair(w.y, left - 2);
+    w.z = mask_pair(w.z, left - 4);
+    w.w = mask_pair(w.w, left - 6);
+}
+template <bool wide> struct BWordOf { using type = uint4; };
+template <> struct BWordOf<false> { using type = uint2; };
 template <typename T> struct EightOf;
 template <> struct EightOf<__half> { using type = uint4; };
 template <> struct EightOf<float> { using type = Eight32; };
@@ -77,11 +91,15 @@ struct Tiles {  // a window's rows in order of their adapters
 };
 
 template <int NR, typename TO>
-__global__ void __launch_bounds__(kT, 2) k_adapters(const AdapterArgs a, int W, int C) {
+__global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterArgs a, int W, int C) {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Tiles s;
     constexpr int kPP = part_pitch<NR>(), kTP = t_pitch<NR>();
+    // A lane of the second product holds eight neighbouring ranks of T and B (two instructions' worth), four where ranks end at 16
+    constexpr bool kWide = NR >= 4;
+    constexpr int kLane = kWide ? 8 : 4;
     using Eight = typename EightOf<TO>::type;
+    using BWord = typename BWordOf<kWide>::type;
     float *part = reinterpret_cast<float *>(smem);
     uint8_t *tsm = smem + smem_bytes<NR>(W) - (size_t)W * kTP;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -149,17 +167,40 @@ __global__ void __launch_bounds__(kT, 2) k_adapters(const AdapterArgs a, int W, 
             const __half *x1 = a.X + (size_t)(m0 + s.row[in1 ? p0 + g + 8 : p0]) * a.ldx + 8 * t;
             const __half *A = a.A + (size_t)s.slot[p0] * a.stride_a + (size_t)g * a.lda + 8 * t;
             const uint4 z = make_uint4(0, 0, 0, 0);
-#pragma unroll 2
-            for (int c = c0 + wk; c < c1; c += slices) {
-                const bool in = c * 32 + 8 * t < a.K;
-                const uint4 u = in && in0 ? *reinterpret_cast<const uint4 *>(x0 + c * 32) : z;
-                const uint4 v = in && in1 ? *reinterpret_cast<const uint4 *>(x1 + c * 32) : z;
+            constexpr int kAhead = 2;  // chunks of X that are on their way while as many are worked on
+            uint4 u[kAhead], v[kAhead];
+            auto load_x = [&](int c) {
 #pragma unroll
-                for (int j = 0; j < NR; ++j) {
-                    if (j * 8 < r) {
-                        const uint4 w = in && j * 8 + g < r ? *reinterpret_cast<const uint4 *>(A + (size_t)j * 8 * a.lda + c * 32) : z;
-                        mma16816(acc[j], u.x, v.x, u.y, v.y, w.x, w.y);
-                        mma16816(acc[j], u.z, v.z, u.w, v.w, w.z, w.w);
+                for (int d = 0; d < kAhead; ++d) {
+                    const int cc = c + d * slices;
+                    const bool in = cc < c1 && cc * 32 + 8 * t < a.K;
+                    u[d] = in && in0 ? *reinterpret_cast<const uint4 *>(x0 + cc * 32) : z;
+                    v[d] = in && in1 ? *reinterpret_cast<const uint4 *>(x1 + cc * 32) : z;
+                }
+            };
+            load_x(c0 + wk);
+            for (int c = c0 + wk; c < c1; c += kAhead * slices) {
+                uint4 xu[kAhead], xv[kAhead];
+#pragma unroll
+                for (int d = 0; d < kAhead; ++d) {
+                    xu[d] = u[d];
+                    xv[d] = v[d];
+                }
+                load_x(c + kAhead * slices);
+#pragma unroll
+                for (int d = 0; d < kAhead; ++d) {
+                    const int cc = c + d * slices;
+                    if (cc >= c1) break;
+                    const bool in = cc * 32 + 8 * t < a.K;
+                    uint4 w[NR];
+#pragma unroll
+                    for (int j = 0; j < NR; ++j) w[j] = in && j * 8 + g < r ? *reinterpret_cast<const uint4 *>(A + (size_t)j * 8 * a.lda + cc * 32) : z;
+#pragma unroll
+                    for (int j = 0; j < NR; ++j) {
+                        if (j * 8 < r) {
+                            mma16816(acc[j], xu[d].x, xv[d].x, xu[d].y, xv[d].y, w[j].x, w[j].y);
+                            mma16816(acc[j], xu[d].z, xv[d].z, xu[d].w, xv[d].w, w[j].z, w[j].w);
+                        }
                     }
                 }
             }
@@ -184,6 +225,41 @@ __global__ void __launch_bounds__(kT, 2) k_adapters(const AdapterArgs a, int W, 
             }
         }
         if (C == 1) __syncthreads();
+    }
+
+    // ---- what the second product reads beside T: on its way before T is there
+    const int chunks = (a.N + 31) >> 5, q0 = (int)((long long)chunks * cta / C), q1 = (int)((long long)chunks * (cta + 1) / C);
+    const int items = tiles * (q1 - q0 > warp ? (q1 - q0 - warp + kWarps - 1) / kWarps : 0);
+    const TO *base = static_cast<const TO *>(a.base);
+    TO *Y = static_cast<TO *>(a.Y);
+    const Eight none{};
+    BWord bw[kWide ? NR / 4 : 1][4];
+    Eight next0 = none, next1 = none;
+    auto load_b = [&](int i, int q) {
+        const int r = s.rank[i];
+        const __half *B = a.B + (size_t)s.slot[s.pos[i]] * a.stride_b + kLane * t;
+#pragma unroll
+        for (int k = 0; k < (kWide ? NR / 4 : 1); ++k) {
+            const int k0 = 4 * kLane * k + kLane * t;  // this lane's first rank
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int col = q * 32 + (g >> 1) * 8 + 2 * j + (g & 1);
+                BWord w{};
+                if (col < a.N && k0 < r) w = *reinterpret_cast<const BWord *>(B + (size_t)col * a.ldb + 4 * kLane * k);
+                if (k0 + kLane > r) mask_beyond(w, r - k0);  // ranks beyond this adapter's own are not looked at
+                bw[k][j] = w;
+            }
+        }
+    };
+    auto load_base = [&](int it) {
+        const int i = it % tiles, p0 = s.pos[i], n = s.count[i], n0 = (q0 + warp + kWarps * (it / tiles)) * 32 + 8 * t;
+        const bool in = base && n0 < a.N;
+        next0 = in && g < n ? *reinterpret_cast<const Eight *>(base + (size_t)(m0 + s.row[p0 + g]) * a.ldbase + n0) : none;
+        next1 = in && g + 8 < n ? *reinterpret_cast<const Eight *>(base + (size_t)(m0 + s.row[p0 + g + 8]) * a.ldbase + n0) : none;
+    };
+    if (items) {
+        load_b(0, q0 + warp);
+        load_base(0);
     }
     if (C > 1) cluster_sync_all();
 
@@ -219,8 +295,9 @@ __global__ void __launch_bounds__(kT, 2) k_adapters(const AdapterArgs a, int W, 
             if (j < NR * 8) {
                 const float x = v[i] * up;
                 const __half hi = __float2half_rn(x), lo = __float2half_rn(x - __half2float(hi));
-                *reinterpret_cast<__half *>(to + (j >> 2) * 16 + (j & 3) * 2) = hi;
-                *reinterpret_cast<__half *>(to + (j >> 2) * 16 + 8 + (j & 3) * 2) = lo;
+                const int at = kWide ? j * 2 : (j >> 2) * 16 + (j & 3) * 2;
+                *reinterpret_cast<__half *>(to + at) = hi;
+                *reinterpret_cast<__half *>(to + at + (kWide ? NR * 16 : 8)) = lo;
             }
         }
         if (lane == 0) s.factor[p] = (a.scale ? a.scale[s.slot[p]] : 1.0f) * down;
@@ -229,50 +306,47 @@ __global__ void __launch_bounds__(kT, 2) k_adapters(const AdapterArgs a, int W, 
     // every CTA has read the others' parts behind this point: waited for at the end
     if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 
-    // ---- Y = base + T B^T: this CTA's part of N
-    const int chunks = (a.N + 31) >> 5, q0 = (int)((long long)chunks * cta / C), q1 = (int)((long long)chunks * (cta + 1) / C);
-    const TO *base = static_cast<const TO *>(a.base);
-    TO *Y = static_cast<TO *>(a.Y);
-    const Eight none{};
-    for (int q = q0 + warp; q < q1; q += kWarps) {
+    // ---- Y = base + T B^T: this CTA's part of N.  A warp takes 32 columns through all tiles: B stays in registers from a tile to the
+    // next of the same adapter, base comes one tile ahead.
+    for (int it = 0; it < items; ++it) {
+        const int i = it % tiles, p0 = s.pos[i], n = s.count[i], r = s.rank[i], q = q0 + warp + kWarps * (it / tiles);
+        if (it && (i == 0 || s.slot[p0] != s.slot[s.pos[i - 1]])) load_b(i, q);
+        const Eight b0 = next0, b1 = next1;
+        if (it + 1 < items) load_base(it + 1);
         const int n0 = q * 32 + 8 * t;
-        const bool in = n0 < a.N;
-        for (int i = 0; i < tiles; ++i) {
-            const int p0 = s.pos[i], n = s.count[i], r = s.rank[i];
-            const bool in0 = in && g < n, in1 = in && g + 8 < n;
-            const size_t r0 = m0 + s.row[in0 ? p0 + g : p0], r1 = m0 + s.row[in1 ? p0 + g + 8 : p0];
-            const Eight b0 = in0 && base ? *reinterpret_cast<const Eight *>(base + r0 * a.ldbase + n0) : none;
-            const Eight b1 = in1 && base ? *reinterpret_cast<const Eight *>(base + r1 * a.ldbase + n0) : none;
-            float acc[4][4];
+        float acc[4][4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
-            const __half *B = a.B + (size_t)s.slot[p0] * a.stride_b + 4 * t;
-            const uint8_t *t0 = tsm + (p0 + (g < n ? g : 0)) * kTP + t * 16, *t1 = tsm + (p0 + (g + 8 < n ? g + 8 : 0)) * kTP + t * 16;
+        for (int j = 0; j < 4; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
+        const int g0 = p0 + (g < n ? g : 0), g1 = p0 + (g + 8 < n ? g + 8 : 0);
+        const uint8_t *t0 = tsm + g0 * kTP + t * 16, *t1 = tsm + g1 * kTP + t * 16;
+        if constexpr (kWide) {
 #pragma unroll
-            for (int k = 0; k < NR / 2; ++k) {
-                if (k * 16 < r) {
-                    const uint4 u = *reinterpret_cast<const uint4 *>(t0 + k * 64), v = *reinterpret_cast<const uint4 *>(t1 + k * 64);
-                    const int k0 = k * 16 + 4 * t;  // this lane's four ranks
+            for (int k = 0; k < NR / 4; ++k) {
+                if (k * 32 < r) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int col = q * 32 + (g >> 1) * 8 + 2 * j + (g & 1);
-                        uint2 w = col < a.N && k0 < r ? *reinterpret_cast<const uint2 *>(B + (size_t)col * a.ldb + k * 16) : make_uint2(0, 0);
-                        if (k0 + 4 > r) {  // ranks beyond this adapter's own are not looked at
-                            if (k0 + 1 >= r) w.x &= 0xffffu;
-                            if (k0 + 2 >= r) w.y = 0;
-                            if (k0 + 3 >= r) w.y &= 0xffffu;
+                    for (int half = 0; half < 2; ++half) {
+                        const uint4 u = *reinterpret_cast<const uint4 *>(t0 + half * (NR * 16) + k * 64);
+                        const uint4 v = *reinterpret_cast<const uint4 *>(t1 + half * (NR * 16) + k * 64);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            mma16816(acc[j], u.x, v.x, u.y, v.y, bw[k][j].x, bw[k][j].y);
+                            mma16816(acc[j], u.z, v.z, u.w, v.w, bw[k][j].z, bw[k][j].w);
                         }
-                        mma16816(acc[j], u.x, v.x, u.y, v.y, w.x, w.y);
-                        mma16816(acc[j], u.z, v.z, u.w, v.w, w.x, w.y);
                     }
                 }
             }
-            const float f0 = s.factor[p0 + (g < n ? g : 0)], f1 = s.factor[p0 + (g + 8 < n ? g + 8 : 0)];
-            const float o0[8] = {acc[0][0], acc[0][1], acc[1][0], acc[1][1], acc[2][0], acc[2][1], acc[3][0], acc[3][1]};
-            const float o1[8] = {acc[0][2], acc[0][3], acc[1][2], acc[1][3], acc[2][2], acc[2][3], acc[3][2], acc[3][3]};
-            if (in0) add_store(Y + r0 * a.ldy + n0, b0, o0, f0);
-            if (in1) add_store(Y + r1 * a.ldy + n0, b1, o1, f1);
+        } else {
+            const uint4 u = *reinterpret_cast<const uint4 *>(t0), v = *reinterpret_cast<const uint4 *>(t1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                mma16816(acc[j], u.x, v.x, u.y, v.y, bw[0][j].x, bw[0][j].y);
+                mma16816(acc[j], u.z, v.z, u.w, v.w, bw[0][j].x, bw[0][j].y);
+            }
         }
+        const float o0[8] = {acc[0][0], acc[0][1], acc[1][0], acc[1][1], acc[2][0], acc[2][1], acc[3][0], acc[3][1]};
+        const float o1[8] = {acc[0][2], acc[0][3], acc[1][2], acc[1][3], acc[2][2], acc[2][3], acc[3][2], acc[3][3]};
+        if (n0 < a.N && g < n) add_store(Y + (size_t)(m0 + s.row[g0]) * a.ldy + n0, b0, o0, s.factor[g0]);
+        if (n0 < a.N && g + 8 < n) add_store(Y + (size_t)(m0 + s.row[g1]) * a.ldy + n0, b1, o1, s.factor[g1]);
     }
     // ---- rows without an adapter
     if (base != Y) {
