@@ -11,15 +11,14 @@
 // The matrix instructions are the ones that read registers (m16n8k16): at ranks up to 64 the operator is bound by X, base and Y in HBM,
 // and operands whose order of k may be chosen freely go from global memory to registers in whole 16-byte words without a
 // detour; n is permuted so that a thread ends up with eight neighbouring results.
-#include <limits.h>
-
 #include "../../include/muxq.h"
-#include "kernels.h"
-#include "ptx.cuh"
+#include "k14_adapters.cuh"
 
 namespace muxq {
 
 namespace {
+
+using namespace adapters;
 
 constexpr int kT = 256, kWarps = kT / 32;
 constexpr int kMostRows = 64;  // of a window
@@ -91,7 +90,7 @@ struct Tiles {  // a window's rows in order of their adapters
 };
 
 template <int NR, typename TO>
-__global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterArgs a, int W, int C) {
+__global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterArgs a, int W, int C, int behind_tiles) {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Tiles s;
     constexpr int kPP = part_pitch<NR>(), kTP = t_pitch<NR>();
@@ -105,23 +104,28 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int cta = C > 1 ? (int)cluster_ctarank() : 0;
     const int m0 = (int)(blockIdx.x / C) * W, rows = min(W, a.M - m0);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // behind the wait: a layer kernel may read its W_q at once
+    if (behind_tiles) {
+        // k_adapter_tiles lets this kernel start behind its own wait, so what both read is there.  It has done this window, or its
+        // rows are not touched by it; either way this kernel must not end before that one has.
+        __shared__ WindowAdapters s_win;
+        int mine;
+        bool bad;
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        if (window_adapters(&s_win, a.row_slot, a.rank, a.slots, a.max_rank, m0 / kWindow * kWindow, a.M, &mine, &bad)) {
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            return;
+        }
+    } else {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // behind the wait: a layer kernel may read its W_q at once
+    }
 
     // ---- rows in order of their adapters, and tiles of up to 16 rows of one adapter
     int key = INT_MAX, rank = 0;
     if (tid < rows) {
-        const int slot = a.row_slot[m0 + tid];
-        bool bad = slot < -1 || slot >= a.slots;
-        if (!bad && slot >= 0) {
-            rank = a.rank ? a.rank[slot] : a.max_rank;
-            bad = rank < 0 || rank > a.max_rank;
-            if (!bad && rank > 0) key = slot;
-        }
-        if (bad) {
-            rank = 0;
-            if (cta == 0) atomicMax(a.dev_status, MUXQ_ERR_INVALID_ARG);
-        }
+        bool bad;
+        key = adapter_of(a.row_slot[m0 + tid], a.rank, a.slots, a.max_rank, &rank, &bad);
+        if (bad && cta == 0) atomicMax(a.dev_status, MUXQ_ERR_INVALID_ARG);
         s.key[tid] = key;
     }
     const int active = __syncthreads_count(key != INT_MAX);
@@ -284,17 +288,15 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        // the largest of the row lands in [2^13, 2^14); a row of nothing but tiny values stays below
-        int e = 13 - ((int)(__float_as_uint(most) >> 23) - 127);
-        if (e > 100 || most == 0.0f) e = most == 0.0f ? 0 : 100;
-        const float up = __uint_as_float((uint32_t)(127 + e) << 23), down = __uint_as_float((uint32_t)(127 - e) << 23);
+        float up, down;
+        row_factors(most, &up, &down);
         uint8_t *to = tsm + p * kTP;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int j = lane + 32 * i;
             if (j < NR * 8) {
-                const float x = v[i] * up;
-                const __half hi = __float2half_rn(x), lo = __float2half_rn(x - __half2float(hi));
+                __half hi, lo;
+                split(v[i] * up, &hi, &lo);
                 const int at = kWide ? j * 2 : (j >> 2) * 16 + (j & 3) * 2;
                 *reinterpret_cast<__half *>(to + at) = hi;
                 *reinterpret_cast<__half *>(to + at + (kWide ? NR * 16 : 8)) = lo;
@@ -358,11 +360,12 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
         }
     }
     __syncwarp();
+    if (behind_tiles) asm volatile("griddepcontrol.wait;" ::: "memory");
     if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 template <int NR, typename TO>
-cudaError_t launch_form(const AdapterArgs &a, int W, int C, cudaStream_t s) {
+cudaError_t launch_form(const AdapterArgs &a, int W, int C, bool behind_tiles, cudaStream_t s) {
     static PerDevice<int> done;
     const int dev = current_device();
     if (dev < 0) return cudaErrorInvalidDevice;
@@ -387,15 +390,15 @@ cudaError_t launch_form(const AdapterArgs &a, int W, int C, cudaStream_t s) {
     attr[1].val.clusterDim.x = C; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = C > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, k_adapters<NR, TO>, a, W, C);
+    return cudaLaunchKernelEx(&cfg, k_adapters<NR, TO>, a, W, C, (int)behind_tiles);
 }
 
 template <typename TO>
-cudaError_t launch_type(const AdapterArgs &a, int W, int C, cudaStream_t s) {
-    if (a.max_rank <= 16) return launch_form<2, TO>(a, W, C, s);
-    if (a.max_rank <= 32) return launch_form<4, TO>(a, W, C, s);
-    if (a.max_rank <= 64) return launch_form<8, TO>(a, W, C, s);
-    return launch_form<16, TO>(a, W, C, s);
+cudaError_t launch_type(const AdapterArgs &a, int W, int C, bool behind_tiles, cudaStream_t s) {
+    if (a.max_rank <= 16) return launch_form<2, TO>(a, W, C, behind_tiles, s);
+    if (a.max_rank <= 32) return launch_form<4, TO>(a, W, C, behind_tiles, s);
+    if (a.max_rank <= 64) return launch_form<8, TO>(a, W, C, behind_tiles, s);
+    return launch_form<16, TO>(a, W, C, behind_tiles, s);
 }
 
 // Rows of a window and CTAs of its cluster.
@@ -415,7 +418,10 @@ cudaError_t launch_adapters(const AdapterArgs &a, cudaStream_t s) {
     if (sms < 1) return cudaErrorInvalidDevice;
     int W, C;
     choose(a, sms, &W, &C);
-    return a.out_f32 ? launch_type<float>(a, W, C, s) : launch_type<__half>(a, W, C, s);
+    cudaError_t e = cudaSuccess;
+    const bool behind_tiles = launch_adapter_tiles(a, s, &e);
+    if (e != cudaSuccess) return e;
+    return a.out_f32 ? launch_type<float>(a, W, C, behind_tiles, s) : launch_type<__half>(a, W, C, behind_tiles, s);
 }
 
 }  // namespace muxq

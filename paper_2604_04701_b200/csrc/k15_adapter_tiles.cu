@@ -1,0 +1,473 @@
+// Low-rank adapters (k14_adapters.cu) on long inputs: windows of 128 rows that hold few adapters, on the tensor cores' own memory.
+//
+// A CTA takes 128 consecutive rows and a range of columns.  X and A come by TMA and T = X A^T is accumulated in tensor memory, for every
+// adapter of the window over all its rows (a row's own T is picked from its adapter's columns).  T is scaled and split into two fp16 halves
+// as in k14_adapters.cu and laid down as the left operand of the second product, which runs over 64 columns of N at a time, again once
+// for every adapter into an accumulator of its own: what an adapter holds reaches no row of another.  base comes by TMA into a ring of
+// tiles, the results are written over it there and leave by TMA, so that no thread addresses global memory and the kernel
+// moves X, base and Y once.  Rows are not sorted: prompts bring an adapter's rows together.
+//
+// Windows that do not suit (too many adapters, a rank that ends inside a step of 16) are left to k_adapters, which runs
+// behind this kernel over all windows and makes the same choice.
+//
+// Roles: warp 0 TMA for X, A, then base; warp 1 products; groups of four warps for the results (one per quarter of the tensor memory's
+// lanes, the first group also for T), steps of N dealt out in turn so that their chains of latencies overlap; the last warp TMA for B.  Every wait is bounded; on expiry the CTA raises MUXQ_ERR_TIMEOUT, lets its copies and products end and returns.
+#include <limits.h>
+
+#include "../../include/muxq.h"
+#include "gemm_common.cuh"
+#include "k14_adapters.cuh"
+
+namespace muxq {
+
+namespace {
+
+using namespace adapters;
+
+constexpr int kGroups = 2;                // of four result warps; a group takes every kGroups-th step of N
+constexpr int kThreads = 32 * (3 + 4 * kGroups), kWarpB = 2 + 4 * kGroups;
+constexpr int kUnit = 64;                 // columns of N at a time
+constexpr int kBox = 128 * 128;           // bytes of 128 rows x 128 bytes
+constexpr int kXStages = 3, kXStage = 2 * kBox;  // X 128 x 64, then A: 128 rows of 64 at most
+constexpr int kTB = 96 * 1024;            // T (32 or 64 KB) and the ring of B
+constexpr int kMaxB = 4, kMaxBase = 8;
+constexpr int kSmem = kTB + 2 * kBox + kXStages * kXStage + 1024;  // + alignment
+
+struct TileParams {
+    int M, K, N, slots, max_rank;
+    const void *base;
+    void *Y;
+    int ldbase, ldy;
+    const int32_t *row_slot, *rank;
+    const float *scale;
+    int32_t *dev_status;
+    uint32_t spin;
+    int skip_chunk;  // -1; a test names a chunk of K whose loads are left out so that a wait runs out
+};
+
+__device__ __forceinline__ void mma_f16_elect(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// fp16 operands, both K-major, fp32 accumulator, 128 rows
+__device__ __forceinline__ uint32_t idesc_f16(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
+__device__ __forceinline__ void tma_load_3d_elect(void *dst, const void *map, uint64_t *bar, int c0, int c1, int c2) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n\t}\n"
+        ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
+        : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_elect(uint64_t *bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}\n"
+        ::"r"(smem_u32(bar))
+        : "memory");
+}
+
+// A window without adapters: this CTA's columns of base.
+template <bool kF32>
+__device__ __forceinline__ void copy_window(const TileParams &p, int m0) {
+    if (p.base == p.Y) return;
+    constexpr int kSize = kF32 ? 4 : 2, kPer = 16 / kSize, kAhead = 4;
+    const int words = p.N / kPer, w0 = (int)((long long)words * blockIdx.y / gridDim.y), n = (int)((long long)words * (blockIdx.y + 1) / gridDim.y) - w0;
+    const int total = min(128, p.M - m0) * n;
+    for (int i = threadIdx.x; i < total; i += kAhead * kThreads) {
+        uint4 v[kAhead];
+        size_t to[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int j = i + k * kThreads, r = j / n, c = w0 + j - r * n;
+            v[k] = make_uint4(0, 0, 0, 0);
+            to[k] = ((size_t)(m0 + r) * p.ldy + (size_t)c * kPer) * kSize;
+            if (j < total && p.base)
+                v[k] = *reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.base) + ((size_t)(m0 + r) * p.ldbase + (size_t)c * kPer) * kSize);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (i + k * kThreads < total) *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.Y) + to[k]) = v[k];
+    }
+}
+
+template <bool kF32>
+__global__ void __launch_bounds__(kThreads, 1)
+k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
+                const __grid_constant__ CUtensorMap tm_base, const __grid_constant__ CUtensorMap tm_y, const TileParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t x_full[kXStages], x_empty[kXStages], b_full[kMaxB], b_empty[kMaxB], base_full[kMaxBase], base_empty[kMaxBase];
+    __shared__ uint64_t t_full, t_ready, acc_full[4], acc_empty[4], drained;
+    __shared__ float s_factor[128];
+    __shared__ WindowAdapters s_win;
+    __shared__ uint32_t s_tmem, s_abort;
+
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const int m0 = blockIdx.x * 128;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // behind the wait: k_adapters may look at the rows at once
+    int mine;
+    bool bad;
+    if (!window_adapters(&s_win, p.row_slot, p.rank, p.slots, p.max_rank, m0, p.M, &mine, &bad)) return;
+    if (bad && blockIdx.y == 0) atomicMax(p.dev_status, MUXQ_ERR_INVALID_ARG);
+    if (s_win.count == 0) {
+        copy_window<kF32>(p, m0);
+        return;
+    }
+    const int d = s_win.count, R8 = p.max_rank, R16 = (R8 + 15) & ~15, R64 = R8 > 64 ? 2 : 1;
+
+    // shared memory: T (upper halves, lower halves) | ring of B | two boxes for base | stages of X and A, later base too
+    const uint32_t base_addr = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *sm = smem_raw + (base_addr - smem_u32(smem_raw));
+    const int t_bytes = R64 * 2 * kBox, b_stage = d * R64 * (kBox / 2);
+    int b_stages = (kTB - t_bytes) / b_stage;
+    if (b_stages > kMaxB) b_stages = kMaxB;
+    constexpr int kBaseStage = kF32 ? 2 * kBox : kBox;
+    constexpr int kBaseStages = (2 * kBox + kXStages * kXStage) / kBaseStage;  // 8, fp32 4
+    constexpr int kBaseEarly = 2 * kBox / kBaseStage;                          // those that do not lie over X and A
+    static_assert(kBaseStages <= kMaxBase, "ring of base");
+    uint8_t *sm_t = sm, *sm_b = sm + t_bytes, *sm_base = sm + kTB, *sm_x = sm_base + 2 * kBox;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kXStages; ++i) { mbar_init(&x_full[i], 1); mbar_init(&x_empty[i], 1); }
+        for (int i = 0; i < kMaxB; ++i) { mbar_init(&b_full[i], 1); mbar_init(&b_empty[i], 1); }
+        for (int i = 0; i < kMaxBase; ++i) { mbar_init(&base_full[i], 1); mbar_init(&base_empty[i], 4); }
+        mbar_init(&t_full, 1);
+        mbar_init(&t_ready, 4);
+        for (int i = 0; i < 4; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4); }
+        mbar_init(&drained, 1);
+        s_abort = 0;
+        fence_barrier_init();
+    }
+    if (warp == 1) {
+        tmem_alloc(&s_tmem, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+    volatile uint32_t *abort_flag = &s_abort;
+    const int bufs = d <= 2 ? 4 : 2, buf_cols = 512 / bufs;  // accumulators: a step of N for every adapter
+    const int chunks = (p.K + 63) >> 6, units = (p.N + kUnit - 1) / kUnit;
+    const int u0 = (int)((long long)units * blockIdx.y / gridDim.y), u1 = (int)((long long)units * (blockIdx.y + 1) / gridDim.y);
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ X and A, then base
+        int issued_x = 0, issued_base = 0;
+        bool ok = true;
+        auto load_base = [&](int k) {
+            const int s = k % kBaseStages;
+            if (!mbar_wait_warp(&base_empty[s], ((k / kBaseStages) & 1) ^ 1, abort_flag, p.spin)) return false;
+            uint8_t *to = sm_base + s * kBaseStage;
+            if (p.base) {
+                mbar_expect_tx_elect(&base_full[s], kBaseStage);
+                tma_load_2d_elect(to, &tm_base, &base_full[s], (u0 + k) * kUnit, m0);
+                if (kF32) tma_load_2d_elect(to + kBox, &tm_base, &base_full[s], (u0 + k) * kUnit + 32, m0);
+            } else {
+                mbar_arrive_elect(&base_full[s]);
+            }
+            return true;
+        };
+        for (; issued_base < kBaseEarly && issued_base < u1 - u0 && ok; ++issued_base) ok = load_base(issued_base);
+        for (; issued_x < chunks && ok; ++issued_x) {
+            const int s = issued_x % kXStages;
+            if (!mbar_wait_warp(&x_empty[s], ((issued_x / kXStages) & 1) ^ 1, abort_flag, p.spin)) { ok = false; break; }
+            if (issued_x == p.skip_chunk) continue;
+            uint8_t *to = sm_x + s * kXStage;
+            mbar_expect_tx_elect(&x_full[s], kBox + d * R8 * 128);
+            tma_load_2d_elect(to, &tm_x, &x_full[s], issued_x * 64, m0);
+            for (int i = 0; i < d; ++i) tma_load_3d_elect(to + kBox + i * R16 * 128, &tm_a, &x_full[s], issued_x * 64, 0, s_win.slot[i]);
+        }
+        // the other tiles of base lie over the stages of X and A: free once the first product is done
+        if (ok) ok = mbar_wait_warp(&t_full, 0, abort_flag, p.spin);
+        for (; issued_base < u1 - u0 && ok; ++issued_base)
+            if (!load_base(issued_base)) { ok = false; break; }
+        if (!ok) {  // every copy that was started lands before the CTA ends
+            for (int k = issued_x > kXStages ? issued_x - kXStages : 0; k < issued_x; ++k)
+                if (k != p.skip_chunk)
+                    for (uint32_t i = 0; i < kSpinLimit; ++i)
+                        if (__all_sync(0xffffffffu, mbar_try_wait(&x_full[k % kXStages], (k / kXStages) & 1))) break;
+            for (int k = issued_base > kBaseStages ? issued_base - kBaseStages : 0; k < issued_base; ++k)
+                for (uint32_t i = 0; i < kSpinLimit; ++i)
+                    if (__all_sync(0xffffffffu, mbar_try_wait(&base_full[k % kBaseStages], (k / kBaseStages) & 1))) break;
+        }
+    } else if (warp == kWarpB) {
+        // ------------------------------------------------------------ B
+        int issued = 0;
+        bool ok = true;
+        for (; issued < u1 - u0 && ok; ++issued) {
+            const int s = issued % b_stages;
+            if (!mbar_wait_warp(&b_empty[s], ((issued / b_stages) & 1) ^ 1, abort_flag, p.spin)) { ok = false; break; }
+            mbar_expect_tx_elect(&b_full[s], b_stage);
+            for (int i = 0; i < d; ++i)
+                for (int k = 0; k < R64; ++k)
+                    tma_load_3d_elect(sm_b + s * b_stage + (i * R64 + k) * (kBox / 2), &tm_b, &b_full[s], k * 64, (u0 + issued) * kUnit, s_win.slot[i]);
+        }
+        if (!ok)
+            for (int k = issued > b_stages ? issued - b_stages : 0; k < issued; ++k)
+                for (uint32_t i = 0; i < kSpinLimit; ++i)
+                    if (__all_sync(0xffffffffu, mbar_try_wait(&b_full[k % b_stages], (k / b_stages) & 1))) break;
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ products
+        bool ok = true;
+        const uint32_t idesc_t = idesc_f16(R16), idesc_y = idesc_f16(kUnit);
+        const uint64_t x_desc = smem_desc_sw128(smem_u32(sm_x));
+        for (int c = 0; c < chunks; ++c) {
+            const int s = c % kXStages;
+            if (!mbar_wait_warp(&x_full[s], (c / kXStages) & 1, abort_flag, p.spin)) { ok = false; break; }
+            tc_fence_after();
+            const uint64_t xd = x_desc + (uint64_t)(s * (kXStage >> 4)), ad = xd + (kBox >> 4);
+            const int steps = min(4, (p.K - c * 64 + 15) >> 4);
+            for (int i = 0; i < d; ++i)
+                for (int k = 0; k < steps; ++k)
+                    mma_f16_elect(tmem + i * R16, xd + 2 * k, ad + (uint64_t)(i * R16 * 8) + 2 * k, idesc_t, c || k ? 1u : 0u);
+            mma_commit_elect(&x_empty[s]);
+        }
+        if (ok) {
+            mma_commit_elect(&t_full);
+            ok = mbar_wait_warp(&t_ready, 0, abort_flag, p.spin);
+            tc_fence_after();
+        }
+        const uint64_t t_desc = smem_desc_sw128(smem_u32(sm_t)), b_desc = smem_desc_sw128(smem_u32(sm_b));
+        for (int u = 0; u < u1 - u0 && ok; ++u) {
+            const int s = u % b_stages, buf = u % bufs;
+            if (!mbar_wait_warp(&acc_empty[buf], ((u / bufs) & 1) ^ 1, abort_flag, p.spin) ||
+                !mbar_wait_warp(&b_full[s], (u / b_stages) & 1, abort_flag, p.spin)) { ok = false; break; }
+            tc_fence_after();
+            for (int i = 0; i < d; ++i) {
+                const int steps = (s_win.rank[i] + 15) >> 4;
+                for (int half = 0; half < 2; ++half)
+                    for (int k = 0; k < steps; ++k) {
+                        const int blk = k >> 2, in = (k & 3) * 2;
+                        mma_f16_elect(tmem + buf * buf_cols + i * kUnit, t_desc + (uint64_t)((half * R64 + blk) * (kBox >> 4)) + in,
+                                      b_desc + (uint64_t)((s * b_stage + (i * R64 + blk) * (kBox / 2)) >> 4) + in, idesc_y, half || k ? 1u : 0u);
+                    }
+            }
+            mma_commit_elect(&b_empty[s]);
+            mma_commit_elect(&acc_full[buf]);
+        }
+        if (!ok) {  // products that are on their way end before their memory is given back
+            mma_commit_elect(&drained);
+            for (uint32_t i = 0; i < kSpinLimit; ++i)
+                if (__all_sync(0xffffffffu, mbar_try_wait(&drained, 0))) break;
+        }
+    } else {
+        // ------------------------------------------------------------ T, then the results
+        const int quad = warp & 3, group = (warp - 2) >> 2, row = quad * 32 + lane;
+        const int own = s_win.index[row];
+        uint32_t present = 0;  // adapters among this warp's rows
+        for (int i = 0; i < d; ++i) present |= __any_sync(0xffffffffu, own == i) ? 1u << i : 0u;
+        const uint32_t taddr = tmem + ((uint32_t)(quad * 32) << 16);
+        bool ok = true;
+        if (group == 0) {
+            ok = mbar_wait_warp(&t_full, 0, abort_flag, p.spin);
+            if (ok) {
+                tc_fence_after();
+                const int r = own >= 0 ? s_win.rank[own] : 0;
+                float most = 0.0f;
+                for (int i = 0; i < d; ++i) {
+                    if (!(present >> i & 1)) continue;
+                    for (int c = 0; c < R16; c += 16) {
+                        uint32_t v[16];
+                        tmem_ld_32x16(taddr + i * R16 + c, v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (own == i && c + j < r) most = fmaxf(most, fabsf(__uint_as_float(v[j])));
+                    }
+                }
+                float up, down;
+                row_factors(most, &up, &down);
+                s_factor[row] = own >= 0 ? (p.scale ? p.scale[s_win.slot[own]] : 1.0f) * down : 0.0f;
+                for (int i = 0; i < d; ++i) {
+                    if (!(present >> i & 1)) continue;
+                    for (int c = 0; c < R16; c += 16) {
+                        uint32_t v[16];
+                        tmem_ld_32x16(taddr + i * R16 + c, v);
+                        tmem_ld_wait();
+                        alignas(16) __half hi[16], lo[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) split(c + j < r ? __uint_as_float(v[j]) * up : 0.0f, &hi[j], &lo[j]);
+                        if (own == i) {
+                            uint8_t *to = sm_t + (c >> 6) * kBox + row * 128;
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const int at = ((((c & 63) >> 3) + k) ^ (row & 7)) * 16;
+                                *reinterpret_cast<uint4 *>(to + at) = *reinterpret_cast<const uint4 *>(hi + 8 * k);
+                                *reinterpret_cast<uint4 *>(to + R64 * kBox + at) = *reinterpret_cast<const uint4 *>(lo + 8 * k);
+                            }
+                        }
+                    }
+                }
+                tc_fence_before();
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&t_ready);
+            }
+        }
+        if (ok) ok = mbar_wait_warp(&t_ready, 0, abort_flag, p.spin);
+        const float f = ok ? s_factor[row] : 0.0f;
+        int last = -1;  // tile of base whose store may still be reading it
+        for (int u = group; u < u1 - u0 && ok; u += kGroups) {
+            const int s = u % kBaseStages, buf = u % bufs;
+            if (!mbar_wait_warp(&acc_full[buf], (u / bufs) & 1, abort_flag, p.spin)) { ok = false; break; }
+            tc_fence_after();
+            uint32_t v[64];
+            const uint32_t from = taddr + buf * buf_cols;
+            if ((present & (present - 1)) == 0) {  // one adapter among these rows, or none
+                const uint32_t at = from + (present ? __ffs(present) - 1 : 0) * kUnit;
+                tmem_ld_32x32(at, *reinterpret_cast<uint32_t(*)[32]>(v));
+                tmem_ld_32x32(at + 32, *reinterpret_cast<uint32_t(*)[32]>(v + 32));
+                tmem_ld_wait();
+            } else {
+                for (int i = 0; i < d; ++i) {
+                    if (!(present >> i & 1)) continue;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        uint32_t w[16];
+                        tmem_ld_32x16(from + i * kUnit + 16 * h, w);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) v[16 * h + j] = own == i ? w[j] : v[16 * h + j];
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&acc_empty[buf]);
+            if (!mbar_wait_warp(&base_full[s], (u / kBaseStages) & 1, abort_flag, p.spin)) { ok = false; break; }
+            uint8_t *tile = sm_base + s * kBaseStage, *at = tile + row * 128;
+            if (own < 0) {  // base as it is
+                if (!p.base)
+                    for (int c = 0; c < kBaseStage / kBox * 8; ++c) *reinterpret_cast<uint4 *>(at + (c >> 3) * kBox + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+            } else if (kF32) {
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                    float4 *q = reinterpret_cast<float4 *>(at + (c >> 3) * kBox + ((c & 7) ^ (row & 7)) * 16);
+                    const float4 b = p.base ? *q : make_float4(0.f, 0.f, 0.f, 0.f);
+                    *q = make_float4(__fmaf_rn(f, __uint_as_float(v[4 * c]), b.x), __fmaf_rn(f, __uint_as_float(v[4 * c + 1]), b.y),
+                                     __fmaf_rn(f, __uint_as_float(v[4 * c + 2]), b.z), __fmaf_rn(f, __uint_as_float(v[4 * c + 3]), b.w));
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    uint4 *q = reinterpret_cast<uint4 *>(at + (c ^ (row & 7)) * 16);
+                    uint4 b = p.base ? *q : make_uint4(0, 0, 0, 0);
+                    __half2 *h = reinterpret_cast<__half2 *>(&b);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 x = __half22float2(h[j]);
+                        h[j] = __floats2half2_rn(__fmaf_rn(f, __uint_as_float(v[8 * c + 2 * j]), x.x), __fmaf_rn(f, __uint_as_float(v[8 * c + 2 * j + 1]), x.y));
+                    }
+                    *q = b;
+                }
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {  // this warp's 32 rows
+                const int col = (u0 + u) * kUnit, r0 = m0 + quad * 32;
+                if (r0 < p.M) {
+                    tma_store_2d(&tm_y, tile + quad * 4096, col, r0);
+                    if (kF32 && col + 32 < p.N) tma_store_2d(&tm_y, tile + kBox + quad * 4096, col + 32, r0);
+                }
+                tma_store_commit();
+                tma_store_wait_read<1>();  // the tile before this one may be loaded over
+                if (last >= 0) mbar_arrive(&base_empty[last]);
+            }
+            last = s;
+            __syncwarp();
+        }
+        if (lane == 0) {
+            tma_store_wait_read<0>();
+            if (ok && last >= 0) mbar_arrive(&base_empty[last]);
+        }
+    }
+    // ---------------------------------------------------------------- teardown
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+    if (threadIdx.x == 0 && s_abort) atomicMax(p.dev_status, MUXQ_ERR_TIMEOUT);
+}
+
+// fp16 or fp32 matrices and stacks of matrices, boxes 128 bytes wide, 128-byte swizzle; what lies outside reads as zero
+bool make_map(CUtensorMap *map, const void *p, bool f32, int dims, const uint64_t (&size)[3], const uint64_t (&pitch)[2], int box_rows) {
+    gemm::EncodeTiledFn fn = gemm::get_encode_fn();
+    if (!fn) return false;
+    const uint64_t esz = f32 ? 4 : 2;
+    cuuint64_t d[3] = {size[0], size[1], size[2]}, st[2] = {pitch[0] * esz, pitch[1] * esz};
+    cuuint32_t box[3] = {(cuuint32_t)(128 / esz), (cuuint32_t)box_rows, 1}, one[3] = {1, 1, 1};
+    return fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, dims, const_cast<void *>(p), d, st, box, one,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool kF32>
+cudaError_t launch_form(const AdapterArgs &a, const CUtensorMap (&m)[5], const TileParams &p, int parts, cudaStream_t s) {
+    static PerDevice<int> done;
+    const int dev = current_device();
+    if (dev < 0) return cudaErrorInvalidDevice;
+    {
+        std::lock_guard<std::mutex> lock(device_mutex());
+        if (!done.have[dev]) {
+            const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(k_adapter_tiles<kF32>), cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+            if (e != cudaSuccess) return e;
+            done.have[dev] = true;
+        }
+    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(((long long)a.M + 127) / 128), parts);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k_adapter_tiles<kF32>, m[0], m[1], m[2], m[3], m[4], p);
+}
+
+constexpr int kMinRows = 1024;
+
+}  // namespace
+
+bool launch_adapter_tiles(const AdapterArgs &a, cudaStream_t s, cudaError_t *e) {
+    const int sms = num_sms();
+    if (a.M < kMinRows || sms < 1) return false;
+    const int64_t far = (int64_t)1 << 38;  // elements; a map's strides end at 2^40 bytes
+    if (a.stride_a > far || a.stride_b > far) return false;
+    CUtensorMap m[5];
+    const bool f32 = a.out_f32;
+    const uint64_t M = a.M, K = a.K, N = a.N, R = a.max_rank, S = a.slots;
+    const uint64_t sa = S > 1 ? (uint64_t)a.stride_a : R * a.lda, sb = S > 1 ? (uint64_t)a.stride_b : N * a.ldb;
+    if (!make_map(&m[0], a.X, false, 2, {K, M, 1}, {(uint64_t)a.ldx, 0}, 128) || !make_map(&m[1], a.A, false, 3, {K, R, S}, {(uint64_t)a.lda, sa}, a.max_rank) ||
+        !make_map(&m[2], a.B, false, 3, {R, N, S}, {(uint64_t)a.ldb, sb}, kUnit) ||
+        !make_map(&m[3], a.base ? a.base : a.Y, f32, 2, {N, M, 1}, {(uint64_t)(a.base ? a.ldbase : a.ldy), 0}, 128) ||
+        !make_map(&m[4], a.Y, f32, 2, {N, M, 1}, {(uint64_t)a.ldy, 0}, 32))
+        return false;
+    TileParams p{};
+    p.M = a.M; p.K = a.K; p.N = a.N; p.slots = a.slots; p.max_rank = a.max_rank;
+    p.row_slot = a.row_slot; p.rank = a.rank; p.scale = a.scale;
+    p.base = a.base; p.Y = a.Y; p.ldbase = a.ldbase; p.ldy = a.ldy;
+    p.dev_status = a.dev_status;
+    p.spin = test_hooks().spin_limit ? test_hooks().spin_limit : kSpinLimit;
+    p.skip_chunk = test_hooks().gemm_skip_kb - 1;
+    const int tiles = (int)(((long long)a.M + 127) / 128), units = (a.N + kUnit - 1) / kUnit;
+    int parts = sms / tiles;
+    if (parts > units) parts = units;
+    if (parts < 1) parts = 1;
+    *e = f32 ? launch_form<true>(a, m, p, parts, s) : launch_form<false>(a, m, p, parts, s);
+    return true;
+}
+
+}  // namespace muxq

@@ -328,6 +328,117 @@ def test_a_request_that_is_not_finite_stays_alone(gpu, value, M):
     assert int(status) == 0
 
 
+def _runs(gen, M, slots, lengths):
+    """Slots of M rows in runs of the given lengths, -1 among them."""
+    ids, i = torch.empty(M, dtype=torch.int64), 0
+    at = 0
+    while at < M:
+        n = lengths[i % len(lengths)]
+        ids[at:at + n] = int(torch.randint(-1, slots, (1,), generator=gen)) if i % 5 else i % slots
+        at, i = at + n, i + 1
+    return ids.int().cuda()
+
+
+# windows of 128 rows with one adapter, with two to four, with more than any window may have, and all of these in one batch
+LENGTHS = {"long": (1000, 333), "short": (70, 61, 90, 20), "few": (33, 32, 40), "mixed": (5, 600, 40, 129, 1, 31, 32, 300)}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", [F16, F32])
+@pytest.mark.parametrize("R,ranks", [(8, None), (16, (16, 0)), (16, (16, 7, 16)), (24, (24, 16)), (32, (32, 16)), (64, (64, 16, 48)), (72, (72, 64)), (128, None), (128, (128, 100, 16, 96))])
+@pytest.mark.parametrize("lengths", sorted(LENGTHS))
+def test_long_inputs(gpu, lengths, R, ranks, out):
+    v, whole = _inputs(1500, 264, 200, 5, R, ranks, out, extra=8)
+    v["ids"] = _runs(torch.Generator().manual_seed(R), 1500, 5, LENGTHS[lengths])
+    _run(gpu, v, whole)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1023, 1024, 1025, 2047, 4097])
+@pytest.mark.parametrize("K,N", [(8, 8), (24, 72), (200, 64), (1288, 136), (64, 1992), (776, 520)])
+def test_long_inputs_of_all_sizes(gpu, M, K, N):
+    """Rows that end inside a window, K and N inside a step; base is Y."""
+    mx = gpu
+    v, whole = _inputs(M, K, N, 3, 16, (16, 16, 9), F32)
+    v["ids"] = _runs(torch.Generator().manual_seed(N), M, 3, (400, 90, 129))
+    want = _run(mx, v, whole).clone()
+    Y, status = v["base"].clone(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    for _ in range(2):
+        Y.copy_(v["base"])
+        mx.muxq_adapters(v["X"], v["A"], v["B"], v["ids"], status, v["scale"], v["rank"], base=Y, out=Y)
+        assert torch.equal(Y, want)
+    v["base"] = None
+    _run(mx, v, whole)
+
+
+@pytest.mark.gpu
+def test_long_inputs_slots_and_ranks_out_of_range(gpu):
+    mx = gpu
+    v, whole = _inputs(2000, 264, 136, 4, 16, (16, 16, 0, 16), F32)
+    v["ids"] = _runs(torch.Generator().manual_seed(3), 2000, 4, (500, 90, 300))
+    _run(mx, v, whole)
+    for bad_id, bad_rank in [(4, None), (-2, None), (2 ** 31 - 1, None), (-2 ** 31, None), (None, 17), (None, -1)]:
+        ids, rank, status = v["ids"].clone(), v["rank"].clone(), torch.zeros(1, dtype=torch.int32, device="cuda")
+        if bad_id is not None:
+            ids[700] = bad_id
+        else:
+            ids[700] = 1
+            rank[1] = bad_rank
+        Y = mx.muxq_adapters(v["X"], v["A"], v["B"], ids, status, v["scale"], rank, v["base"])
+        assert int(status) == mx.MUXQ_ERR_INVALID_ARG
+        changed = torch.arange(2000, device="cuda") == 700 if bad_id is not None else ids == 1
+        assert torch.equal(Y[changed], v["base"][changed])
+        check(Y, *reference(v["X"], v["A"], v["B"], ids, v["scale"], rank, v["base"]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_long_inputs_that_are_not_finite_stay_alone(gpu, value):
+    """Adapters of one window do not reach each other's rows, whatever they hold."""
+    mx = gpu
+    v, whole = _inputs(1300, 264, 136, 4, 16, None, F32)
+    v["ids"] = _runs(torch.Generator().manual_seed(5), 1300, 4, (50, 70, 128, 30))
+    good, status = _run(mx, v, whole).clone(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    row = int((v["ids"] >= 0).nonzero()[0])
+    X = v["X"].clone()
+    X[row, 77] = value
+    Y = mx.muxq_adapters(X, v["A"], v["B"], v["ids"], status, v["scale"], None, v["base"])
+    keep = torch.arange(1300, device="cuda") != row
+    assert torch.equal(Y[keep], good[keep])
+    for which in ("A", "B"):
+        w = {k: v[k].clone() for k in ("A", "B")}
+        w[which][2, 5, 7] = value
+        Y = mx.muxq_adapters(v["X"], w["A"], w["B"], v["ids"], status, v["scale"], None, v["base"])
+        assert torch.equal(Y[v["ids"] != 2], good[v["ids"] != 2])
+    base = v["base"].clone()
+    base[::7, 3] = value
+    Y = mx.muxq_adapters(v["X"], v["A"], v["B"], v["ids"], status, v["scale"], None, base)
+    keep = torch.ones(1300, 136, dtype=torch.bool, device="cuda")
+    keep[::7, 3] = False
+    assert torch.equal(Y[keep], good[keep]) and not torch.isfinite(Y[~keep]).any()
+
+
+@pytest.mark.gpu
+def test_long_inputs_time_out(gpu):
+    """A wait that runs out (the loads of a part of K are left out by a test hook) ends the kernel with a status; the next call is right."""
+    mx = gpu
+    v, whole = _inputs(1500, 776, 200, 2, 32, None, F16)
+    v["ids"].fill_(1)
+    want = _run(mx, v, whole).clone()
+    before = whole.clone()
+    for chunk in (1, 5, 12):
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        mx.muxq_test_hooks(spin_limit=20000, gemm_skip_k_block=chunk)
+        try:
+            mx.muxq_adapters(v["X"], v["A"], v["B"], v["ids"], status, v["scale"], None, v["base"], out=whole[:1500, :200])
+            torch.cuda.synchronize()
+        finally:
+            mx.muxq_test_hooks()
+        assert int(status) == mx.MUXQ_ERR_TIMEOUT
+        assert torch.equal(whole[1500:], before[1500:])
+        assert torch.equal(_run(mx, v, whole), want)
+
+
 @pytest.mark.gpu
 def test_an_adapter_loaded_ahead_of_the_call(gpu):
     """Slots are rewritten and rows reassigned between the replays of one graph, and by work directly ahead on the stream."""
