@@ -590,7 +590,7 @@ int muxq_residual_norm(const void *R, int ldr, int res_kind, const void *Y, int 
     a.R = R; a.ldr = ldr; a.res_f32 = res_kind == MUXQ_OUT_F32;
     a.Y = Y; a.ldy = ldy; a.y_f32 = Y && y_kind == MUXQ_OUT_F32;
     a.gate = gate; a.ldg = ldg; a.gate_f32 = gate_kind == MUXQ_OUT_F32; a.gate_group = gate_group;
-    a.alpha = alpha;
+    a.alpha = alpha; a.inv_d = 1.0f / (float)D;
     a.M = M; a.D = D;
     a.H = H; a.ldh = ldh;
     a.X = static_cast<__half *>(X); a.ldx = ldx;

@@ -15,10 +15,11 @@ namespace {
 
 constexpr int kMaxThreads = 512;  // of a row
 constexpr int kMostUnits = 10;    // of four channels, per thread
-constexpr int kEarlyUnits = 3;    // up to here a thread fetches vectors and gate together with its row
+constexpr int kGateUnits = 6;     // up to here it fetches a gate by rows together with its row
+constexpr int kEarlyUnits = 3;    // up to here the vectors too
 
 struct RowSum {  // sums over the threads of a row; every call has a place of its own in shared memory, so one barrier is enough
-    float *red;      // [4][16] of this row
+    float *red;      // [4][16]
     int warps, warp, lane, at;
     __device__ __forceinline__ float operator()(float v) {
 #pragma unroll
@@ -42,142 +43,193 @@ template <typename T>
 __device__ __forceinline__ typename RawOf<T>::type load4(const T *p) {
     return *reinterpret_cast<const typename RawOf<T>::type *>(p);
 }
-__device__ __forceinline__ float4 floats(const uint2 &v) {
-    const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&v.x)), b = __half22float2(*reinterpret_cast<const __half2 *>(&v.y));
-    return make_float4(a.x, a.y, b.x, b.y);
+struct Four {  // four neighbouring channels as two pairs: the packed instructions on pairs halve what there is to issue
+    float2 a, b;
+};
+__device__ __forceinline__ Four four(const uint2 &v) {
+    return Four{__half22float2(*reinterpret_cast<const __half2 *>(&v.x)), __half22float2(*reinterpret_cast<const __half2 *>(&v.y))};
 }
-__device__ __forceinline__ float4 floats(const uint4 &v) {
-    return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+__device__ __forceinline__ Four four(const uint4 &v) {
+    return Four{make_float2(__uint_as_float(v.x), __uint_as_float(v.y)), make_float2(__uint_as_float(v.z), __uint_as_float(v.w))};
 }
-__device__ __forceinline__ void store4(__half *p, const float4 &v) {
-    const __half2 a = __floats2half2_rn(v.x, v.y), b = __floats2half2_rn(v.z, v.w);
+__device__ __forceinline__ Four four(float x) { return Four{make_float2(x, x), make_float2(x, x)}; }
+__device__ __forceinline__ Four load_vec(const float *p) { return four(load4(p)); }
+__device__ __forceinline__ Four operator*(const Four &x, const Four &y) { return Four{__fmul2_rn(x.a, y.a), __fmul2_rn(x.b, y.b)}; }
+__device__ __forceinline__ Four operator+(const Four &x, const Four &y) { return Four{__fadd2_rn(x.a, y.a), __fadd2_rn(x.b, y.b)}; }
+__device__ __forceinline__ Four fma4(const Four &x, const Four &y, const Four &z) { return Four{__ffma2_rn(x.a, y.a, z.a), __ffma2_rn(x.b, y.b, z.b)}; }
+__device__ __forceinline__ void store4(__half *p, const Four &v) {
+    const __half2 a = __float22half2_rn(v.a), b = __float22half2_rn(v.b);
     *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
 }
-__device__ __forceinline__ void store4(float *p, const float4 &v) { *reinterpret_cast<float4 *>(p) = v; }
+__device__ __forceinline__ void store4(float *p, const Four &v) { *reinterpret_cast<float4 *>(p) = make_float4(v.a.x, v.a.y, v.b.x, v.b.y); }
 
-// v <- norm of the row v, without weight and bias.  Units beyond the row hold zeros and keep them.
+// The differences from the row's mean where the norm wants them, and the factor that norms them.  A unit beyond the row (only a thread's last
+// can be one) holds zeros and keeps them.
 template <int V>
-__device__ __forceinline__ void normalize(float4 (&v)[V], const NormSpec &n, int D, int units, int T, int t, RowSum &sum) {
-    const float inv_d = __fdiv_rn(1.0f, (float)D);
+__device__ __forceinline__ Four normalize(Four (&v)[V], const NormSpec &n, float inv_d, bool last_in, RowSum &sum) {
     if (n.kind == MUXQ_NORM_LAYER) {
-        float s = 0.0f;
+        Four s = v[0];
 #pragma unroll
-        for (int i = 0; i < V; ++i) s += (v[i].x + v[i].y) + (v[i].z + v[i].w);
-        const float mu = sum(s) * inv_d;
+        for (int i = 1; i < V; ++i) s = s + v[i];
+        const Four minus = four(-(sum((s.a.x + s.a.y) + (s.b.x + s.b.y)) * inv_d));
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (t + i * T < units) { v[i].x -= mu; v[i].y -= mu; v[i].z -= mu; v[i].w -= mu; }
+        for (int i = 0; i < V - 1; ++i) v[i] = v[i] + minus;
+        if (last_in) v[V - 1] = v[V - 1] + minus;
     }
-    float q = 0.0f;
+    Four q = v[0] * v[0];
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-        q += __fmaf_rn(v[i].x, v[i].x, v[i].y * v[i].y) + __fmaf_rn(v[i].z, v[i].z, v[i].w * v[i].w);
-    const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fmaf_rn(sum(q), inv_d, n.eps)));
-#pragma unroll
-    for (int i = 0; i < V; ++i) { v[i].x *= r; v[i].y *= r; v[i].z *= r; v[i].w *= r; }
+    for (int i = 1; i < V; ++i) q = fma4(v[i], v[i], q);
+    return four(rsqrtf(__fmaf_rn(sum((q.a.x + q.a.y) + (q.b.x + q.b.y)), inv_d, n.eps)));  // (off by 2 units at most)
 }
 
-__device__ __forceinline__ void scale_shift(float4 &v, const float4 &w, const float4 &b) {
-    v.x = __fmaf_rn(v.x, w.x, b.x); v.y = __fmaf_rn(v.y, w.y, b.y); v.z = __fmaf_rn(v.z, w.z, b.z); v.w = __fmaf_rn(v.w, w.w, b.w);
+// v <- v r weight + bias; the vectors come from memory where they have not been fetched ahead
+template <int V>
+__device__ __forceinline__ void scale_shift(Four (&v)[V], const Four &r, const float *weight, const float *bias, uint32_t c, uint32_t step, bool last_in) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = v[i] * r;
+    if (weight) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < V - 1 || last_in) v[i] = v[i] * load_vec(weight + (c + i * step));
+    }
+    if (bias) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < V - 1 || last_in) v[i] = v[i] + load_vec(bias + (c + i * step));
+    }
+}
+template <int V>
+__device__ __forceinline__ void scale_shift(Four (&v)[V], const Four &r, const Four (&weight)[V], const Four (&bias)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = fma4(v[i] * r, weight[i], bias[i]);
+}
+template <int V>
+__device__ __forceinline__ void fetch(Four (&to)[V], const float *p, float none, uint32_t c, uint32_t step, bool last_in) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) to[i] = p && (i < V - 1 || last_in) ? load_vec(p + (c + i * step)) : four(none);
 }
 
 template <int V, typename TR, typename TY>
-__global__ void __launch_bounds__(kMaxThreads) k_residual_norm(const ResidualNormArgs a, int T) {
-    __shared__ float s_red[kMaxThreads / 32][4][16];
-    const int sub = threadIdx.x / T, t = threadIdx.x - sub * T;
-    const int rows = blockDim.x / T, units = a.D >> 2;
-    const int m = blockIdx.x * rows + sub;
-    const bool have = m < a.M;  // (rows behind the last one go along to the barriers)
-    RowSum sum{&s_red[sub][0][0], T >> 5, t >> 5, t & 31, 0};
-    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f), one = make_float4(1.f, 1.f, 1.f, 1.f);
+__global__ void __maxnreg__(V > 6 ? 128 : sizeof(TR) == 4 ? 112 : 96) k_residual_norm(const ResidualNormArgs a) {
+    __shared__ float s_red[4][16];
+    const int t = threadIdx.x, T = blockDim.x;
+    const int m = blockIdx.x * blockDim.y + threadIdx.y;
+    if (m >= a.M) return;  // (a row of several warps has its CTA to itself)
+    RowSum sum{&s_red[0][0], T >> 5, t >> 5, t & 31, 0};
+    // this thread's channels: four from c on, then every `step` further; all but the last four are within the row
+    const uint32_t c = 4 * t, step = 4 * T;
+    const bool last_in = c + (V - 1) * step < (uint32_t)a.D;
+    const size_t row = m;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // behind the wait: a layer kernel may read its W_q at once
-    const TR *R = static_cast<const TR *>(a.R) + (size_t)m * a.ldr;
-    const TY *Y = static_cast<const TY *>(a.Y) + (size_t)m * a.ldy;
-    const size_t grow = a.gate_group ? (size_t)(m / a.gate_group) * a.ldg : 0;
-    auto vec = [&](const float *p, int i, const float4 &none) {
-        return p && t + i * T < units ? *reinterpret_cast<const float4 *>(p + 4 * (t + i * T)) : none;
-    };
-    auto gate = [&](int i) {
-        if (!a.gate || t + i * T >= units || !have) return one;
-        const size_t at = grow + 4 * (t + i * T);
-        return a.gate_f32 ? floats(load4(static_cast<const float *>(a.gate) + at)) : floats(load4(static_cast<const __half *>(a.gate) + at));
-    };
-    typename RawOf<TR>::type r[V];
-    typename RawOf<TY>::type yr[V];
-    const typename RawOf<TR>::type rz{};
-    const typename RawOf<TY>::type yz{};
+    using RawR = typename RawOf<TR>::type;
+    using RawY = typename RawOf<TY>::type;
+    RawR r[V];
+    RawY yr[V];
+    if (a.R) {
+        const TR *R = static_cast<const TR *>(a.R) + row * a.ldr;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const bool in = have && t + i * T < units;
-        r[i] = in && a.R ? load4(R + 4 * (t + i * T)) : rz;
-        yr[i] = in && a.Y ? load4(Y + 4 * (t + i * T)) : yz;
-    }
-    constexpr bool kEarly = V <= kEarlyUnits;
-    float4 wp[kEarly ? V : 1], bp[kEarly ? V : 1], gt[kEarly ? V : 1], wn[kEarly ? V : 1], bn[kEarly ? V : 1];
-    if constexpr (kEarly) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            wp[i] = vec(a.post.weight, i, one); bp[i] = vec(a.post.bias, i, zero);
-            gt[i] = gate(i);
-            wn[i] = vec(a.pre.weight, i, one); bn[i] = vec(a.pre.bias, i, zero);
-        }
-    }
-    float4 h[V];
-    if (a.Y) {
-        float4 y[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) y[i] = floats(yr[i]);
-        if (a.post.kind != MUXQ_NORM_NONE) {
-            normalize(y, a.post, a.D, units, T, t, sum);
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                scale_shift(y[i], kEarly ? wp[kEarly ? i : 0] : vec(a.post.weight, i, one), kEarly ? bp[kEarly ? i : 0] : vec(a.post.bias, i, zero));
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float4 g = kEarly ? gt[kEarly ? i : 0] : gate(i), f = floats(r[i]);
-            h[i].x = __fmaf_rn(a.alpha, y[i].x * g.x, f.x);
-            h[i].y = __fmaf_rn(a.alpha, y[i].y * g.y, f.y);
-            h[i].z = __fmaf_rn(a.alpha, y[i].z * g.z, f.z);
-            h[i].w = __fmaf_rn(a.alpha, y[i].w * g.w, f.w);
-        }
+        for (int i = 0; i < V; ++i) r[i] = i < V - 1 || last_in ? load4(R + (c + i * step)) : RawR{};
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) h[i] = floats(r[i]);
+        for (int i = 0; i < V; ++i) r[i] = RawR{};
     }
-    if (a.H && have) {
-        TR *H = static_cast<TR *>(a.H) + (size_t)m * a.ldh;
+    if (a.Y) {
+        const TY *Y = static_cast<const TY *>(a.Y) + row * a.ldy;
+#pragma unroll
+        for (int i = 0; i < V; ++i) yr[i] = i < V - 1 || last_in ? load4(Y + (c + i * step)) : RawY{};
+    }
+    // A gate by rows is as many bytes as Y, and on its way with the row, as it stands in memory.
+    constexpr bool kGateAhead = V <= kGateUnits;
+    const float *gate32 = static_cast<const float *>(a.gate);
+    const __half *gate16 = static_cast<const __half *>(a.gate);
+    if (a.gate && a.gate_group) {
+        const size_t at = (size_t)(a.gate_group == 1 ? (uint32_t)row : (uint32_t)row / (uint32_t)a.gate_group) * a.ldg;
+        gate32 += at;
+        gate16 += at;
+    }
+    uint4 gr[kGateAhead ? V : 1];
+    if (kGateAhead && a.gate) {
+        if (a.gate_f32) {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (i < V - 1 || last_in) gr[kGateAhead ? i : 0] = load4(gate32 + (c + i * step));
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (i < V - 1 || last_in) {
+                    const uint2 v = load4(gate16 + (c + i * step));
+                    gr[kGateAhead ? i : 0].x = v.x;
+                    gr[kGateAhead ? i : 0].y = v.y;
+                }
+        }
+    }
+    constexpr bool kEarly = V <= kEarlyUnits;
+    Four wp[kEarly ? V : 1], bp[kEarly ? V : 1], wn[kEarly ? V : 1], bn[kEarly ? V : 1];
+    if constexpr (kEarly) {
+        fetch(wp, a.post.weight, 1.0f, c, step, last_in);
+        fetch(bp, a.post.bias, 0.0f, c, step, last_in);
+        fetch(wn, a.pre.weight, 1.0f, c, step, last_in);
+        fetch(bn, a.pre.bias, 0.0f, c, step, last_in);
+    }
+    Four h[V];
+    if (a.Y) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) h[i] = four(yr[i]);
+        if (a.post.kind != MUXQ_NORM_NONE) {
+            const Four by = normalize(h, a.post, a.inv_d, last_in, sum);
+            if constexpr (kEarly) scale_shift(h, by, wp, bp);
+            else scale_shift(h, by, a.post.weight, a.post.bias, c, step, last_in);
+        }
+        if (a.gate) {
+            if (a.gate_f32) {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (i < V - 1 || last_in) h[i] = h[i] * (kGateAhead ? four(gr[kGateAhead ? i : 0]) : four(load4(gate32 + (c + i * step))));
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (i < V - 1 || last_in)
+                        h[i] = h[i] * (kGateAhead ? four(make_uint2(gr[kGateAhead ? i : 0].x, gr[kGateAhead ? i : 0].y)) : four(load4(gate16 + (c + i * step))));
+            }
+        }
+        const Four alpha = four(a.alpha);
+#pragma unroll
+        for (int i = 0; i < V; ++i) h[i] = fma4(alpha, h[i], four(r[i]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) h[i] = four(r[i]);
+    }
+    if (a.H) {
+        TR *H = static_cast<TR *>(a.H) + row * a.ldh;
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (t + i * T < units) store4(H + 4 * (t + i * T), h[i]);
+            if (i < V - 1 || last_in) store4(H + (c + i * step), h[i]);
     }
     if (!a.X) return;
     if (a.pre.kind != MUXQ_NORM_NONE) {
-        normalize(h, a.pre, a.D, units, T, t, sum);
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            scale_shift(h[i], kEarly ? wn[kEarly ? i : 0] : vec(a.pre.weight, i, one), kEarly ? bn[kEarly ? i : 0] : vec(a.pre.bias, i, zero));
+        const Four by = normalize(h, a.pre, a.inv_d, last_in, sum);
+        if constexpr (kEarly) scale_shift(h, by, wn, bn);
+        else scale_shift(h, by, a.pre.weight, a.pre.bias, c, step, last_in);
     }
-    if (!have) return;
-    __half *X = a.X + (size_t)m * a.ldx;
+    __half *X = a.X + row * a.ldx;
 #pragma unroll
     for (int i = 0; i < V; ++i)
-        if (t + i * T < units) store4(X + 4 * (t + i * T), h[i]);
+        if (i < V - 1 || last_in) store4(X + (c + i * step), h[i]);
 }
 
 template <int V, typename TR, typename TY>
 cudaError_t launch_form(const ResidualNormArgs &a, int T, int rows, cudaStream_t s) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(((long long)a.M + rows - 1) / rows));
-    cfg.blockDim = dim3(T * rows);
+    cfg.blockDim = dim3(T, rows);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_residual_norm<V, TR, TY>, a, T);
+    return cudaLaunchKernelEx(&cfg, k_residual_norm<V, TR, TY>, a);
 }
 
 template <typename TR, typename TY>
@@ -187,8 +239,11 @@ cudaError_t launch_types(const ResidualNormArgs &a, int V, int T, int rows, cuda
         case 2: return launch_form<2, TR, TY>(a, T, rows, s);
         case 3: return launch_form<3, TR, TY>(a, T, rows, s);
         case 4: return launch_form<4, TR, TY>(a, T, rows, s);
-        case 5: case 6: return launch_form<6, TR, TY>(a, T, rows, s);
-        case 7: case 8: return launch_form<8, TR, TY>(a, T, rows, s);
+        case 5: return launch_form<5, TR, TY>(a, T, rows, s);
+        case 6: return launch_form<6, TR, TY>(a, T, rows, s);
+        case 7: return launch_form<7, TR, TY>(a, T, rows, s);
+        case 8: return launch_form<8, TR, TY>(a, T, rows, s);
+        case 9: return launch_form<9, TR, TY>(a, T, rows, s);
         default: return launch_form<kMostUnits, TR, TY>(a, T, rows, s);
     }
 }
@@ -198,14 +253,15 @@ cudaError_t launch_types(const ResidualNormArgs &a, int V, int T, int rows, cuda
 cudaError_t launch_residual_norm(const ResidualNormArgs &a, cudaStream_t s) {
     const int units = a.D >> 2, sms = num_sms();
     if (sms < 1) return cudaErrorInvalidDevice;
-    // few rows: as many threads as leave a unit or two to each; many: as few as can hold a row
-    int T;
-    if ((long long)a.M <= 4 * sms) T = ((units + 1) / 2 + 31) / 32 * 32;
-    else T = ((units + kMostUnits - 1) / kMostUnits + 31) / 32 * 32;
+    // Few rows: as many threads as leave a unit or two to each.  Many: as few as can hold a row in their registers, one warp as long as it can;
+    // an SM then holds enough rows that one's loads go on under another's sums (us, one warp / two / four: 8192 x 768 11.6 / 15.6 / 24.1,
+    // 16384 x 1280 with a gate by rows 47.9 / 51.2 / 66.7; two / four: 2000 x 2560 12.7 / 12.8; 300 x 1280 3.2 / 3.2 / 2.9).
+    const bool few = (long long)a.M <= 4 * sms;
+    int T = few ? ((units + 1) / 2 + 31) / 32 * 32 : 32;
+    while (!few && T * kMostUnits < units) T *= 2;
     if (T > kMaxThreads) T = kMaxThreads;
     const int V = (units + T - 1) / T;
-    int rows = (long long)a.M <= 4 * sms ? 1 : 256 / T;
-    if (rows < 1) rows = 1;
+    const int rows = T == 32 ? 2 : 1;
     if (a.res_f32) return a.y_f32 ? launch_types<float, float>(a, V, T, rows, s) : launch_types<float, __half>(a, V, T, rows, s);
     return a.y_f32 ? launch_types<__half, float>(a, V, T, rows, s) : launch_types<__half, __half>(a, V, T, rows, s);
 }

@@ -310,7 +310,7 @@ struct ResidualNormArgs {
     const void *gate;    // NULL: 1
     int ldg, gate_f32;
     int gate_group;      // rows that share a row of the gate; 0: all
-    float alpha;
+    float alpha, inv_d;  // inv_d: 1 / D
     int M, D;
     void *H;             // type of R, or NULL
     int ldh;
