@@ -31,15 +31,29 @@ def _deps_mtime():
     return max(os.path.getmtime(p) for p in paths)
 
 
+def build_calls() -> None:
+    """_calls.so: py_calls.c, and py_tensor.cpp against the headers and libraries of the torch that is installed."""
+    import torch
+    home = os.path.dirname(torch.__file__)
+    flags = ["-O2", "-Wall", "-fPIC", "-I" + sysconfig.get_paths()["include"]]
+    objs = [os.path.join(OBJ_DIR, f) for f in ("py_calls.o", "py_tensor.o")]
+    subprocess.check_call([os.environ.get("CC", "gcc"), *flags, "-c", os.path.join(CSRC, "py_calls.c"), "-o", objs[0]])
+    cxx = os.environ.get("CXX", "g++")
+    subprocess.check_call([cxx, *flags, "-std=c++17", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+                           *("-isystem" + os.path.join(home, "include", d) for d in ("", "torch/csrc/api/include")),
+                           "-c", os.path.join(CSRC, "py_tensor.cpp"), "-o", objs[1]])
+    tmp = CALLS + f".tmp{os.getpid()}"
+    libs = os.path.join(home, "lib")
+    subprocess.check_call([cxx, "-shared", *objs, "-L" + libs, "-Wl,-rpath," + libs, "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", tmp])
+    os.replace(tmp, CALLS)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and all(os.path.exists(f) and os.path.getmtime(f) >= _deps_mtime() for f in (LIB, CALLS)):
         return LIB
-    tmp = CALLS + f".tmp{os.getpid()}"
-    subprocess.check_call([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"],
-                           os.path.join(CSRC, "py_calls.c"), "-o", tmp])
-    os.replace(tmp, CALLS)
-    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     os.makedirs(OBJ_DIR, exist_ok=True)
+    build_calls()
+    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     srcs = _sources()
     objs = [os.path.join(OBJ_DIR, os.path.basename(s)[:-3] + ".o") for s in srcs]
 

@@ -10,6 +10,7 @@
 #include <string.h>
 
 #include "../../include/muxq.h"
+#include "py_tensor.h"
 
 typedef int (*linear_fn)(const void *, int, int, int, const int8_t *, int, const float *, int, const muxq_params *, void *,
                          int, int, void *, size_t, int32_t *, void *);
@@ -200,43 +201,72 @@ static PyObject *quantize_weight(PyObject *self, PyObject *const *a, Py_ssize_t 
 }
 
 /* A tensor as an operand, with what is wanted of it checked.  `what` stands in the message. */
-typedef struct {
-    void *ptr;
-    int kind, rows, cols, ld, dim; /* kind: MUXQ_OUT_F16 or MUXQ_OUT_F32; one dimension: rows = 1 */
-} operand;
 static int refuse(const char *what, const char *why) {
     PyErr_Format(PyExc_ValueError, "%s: %s", what, why);
     return -1;
 }
-static int operand_of(PyObject *t, const char *what, int device, int dims, operand *o) { /* dims: 1, 2, or 3 for either */
-    int at = -1, second = 0, sa, sb, f16, f32;
-    if (as_int(PyObject_CallMethodNoArgs(t, n_get_device), &at)) return -1;
-    if (at < 0) return refuse(what, "a CUDA tensor is wanted");
-    if (at != device) return refuse(what, "the tensor is on another device than the current one");
-    if ((f16 = has_dtype(t, dt_f16)) < 0 || (f32 = has_dtype(t, dt_f32)) < 0) return -1;
-    if (!f16 && !f32) return refuse(what, "fp16 or fp32 is wanted");
-    o->kind = f16 ? MUXQ_OUT_F16 : MUXQ_OUT_F32;
-    if (shape_of(t, &o->rows, &second, &o->dim) || stride_of(t, &sa, &sb)) return -1;
-    if (o->dim > 2 || !(dims & o->dim)) return refuse(what, "the number of dimensions is not what is wanted");
-    if (o->dim == 1) {
-        second = o->rows;
-        o->rows = 1;
-        sb = sa;
+/* the same of an object that only behaves like a tensor */
+static int info_by_attributes(PyObject *t, tensor_info *o) {
+    if (as_int(PyObject_CallMethodNoArgs(t, n_get_device), &o->device)) return -1;
+    PyObject *dt = PyObject_GetAttr(t, n_dtype), *shape = dt ? PyObject_GetAttr(t, n_shape) : NULL, *st = shape ? PyObject_CallMethodNoArgs(t, n_stride) : NULL;
+    int rc = st ? 0 : -1;
+    if (!rc) {
+        o->dtype = dt == dt_f16 ? TENSOR_F16 : dt == dt_f32 ? TENSOR_F32 : dt == dt_i32 ? TENSOR_I32 : TENSOR_OTHER;
+        o->dim = -1;
+        if (PyTuple_Check(shape) && PyTuple_Check(st) && PyTuple_GET_SIZE(shape) == PyTuple_GET_SIZE(st)) o->dim = (int)PyTuple_GET_SIZE(shape);
+        for (int i = 0; i < o->dim && i < 3 && !rc; ++i) {
+            o->size[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i));
+            o->stride[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(st, i));
+            rc = PyErr_Occurred() ? -1 : 0;
+        }
     }
-    o->cols = second;
-    if (second > 1 && sb != 1) return refuse(what, "unit stride along the last dimension is wanted");
-    o->ld = o->rows == 1 ? o->cols : sa; /* (the stride of a dimension of one says nothing) */
-    return tensor_ptr(t, &o->ptr);
+    Py_XDECREF(dt);
+    Py_XDECREF(shape);
+    Py_XDECREF(st);
+    return rc ? -1 : tensor_ptr(t, &o->ptr);
+}
+/* a CUDA tensor on the current device with unit stride along its last dimension */
+static int cuda_info(PyObject *t, const char *what, int device, int dims, tensor_info *o) { /* dims: bit d for d dimensions */
+    const int rc = tensor_info_of(t, o);
+    if (rc < 0 || (!rc && info_by_attributes(t, o))) return -1;
+    if (o->device < 0) return refuse(what, "a CUDA tensor is wanted");
+    if (o->device != device) return refuse(what, "the tensor is on another device than the current one");
+    if (o->dim < 1 || o->dim > 3 || !(dims >> o->dim & 1)) return refuse(what, "the number of dimensions is not what is wanted");
+    for (int i = 0; i < o->dim; ++i)
+        if (o->size[i] > INT32_MAX) return refuse(what, "a dimension does not fit a C int");
+    if (o->size[o->dim - 1] > 1 && o->stride[o->dim - 1] != 1) return refuse(what, "unit stride along the last dimension is wanted");
+    return 0;
+}
+static int pitch_of(const tensor_info *o, int dim, const char *what, int *ld) { /* (the stride of a dimension of one says nothing) */
+    const int64_t v = o->size[dim] == 1 ? o->size[dim + 1] : o->stride[dim];
+    if (v > INT32_MAX || v < 0) return refuse(what, "a pitch does not fit a C int");
+    *ld = (int)v;
+    return 0;
+}
+typedef struct {
+    void *ptr;
+    int kind, rows, cols, ld, dim; /* kind: MUXQ_OUT_F16 or MUXQ_OUT_F32; one dimension: rows = 1 */
+} operand;
+static int operand_of(PyObject *t, const char *what, int device, int dims, operand *o) {
+    tensor_info v = {0};
+    if (cuda_info(t, what, device, dims, &v)) return -1;
+    if (v.dtype != TENSOR_F16 && v.dtype != TENSOR_F32) return refuse(what, "fp16 or fp32 is wanted");
+    o->ptr = v.ptr;
+    o->kind = v.dtype == TENSOR_F16 ? MUXQ_OUT_F16 : MUXQ_OUT_F32;
+    o->dim = v.dim;
+    o->rows = v.dim == 1 ? 1 : (int)v.size[0];
+    o->cols = o->ld = (int)v.size[v.dim - 1];
+    return v.dim == 1 ? 0 : pitch_of(&v, 0, what, &o->ld);
 }
 static int matrix_of(PyObject *t, const char *what, int device, int rows, int cols, operand *o) {
-    if (operand_of(t, what, device, 2, o)) return -1;
+    if (operand_of(t, what, device, 1 << 2, o)) return -1;
     return o->rows == rows && o->cols == cols ? 0 : refuse(what, "the shape does not fit the other operands");
 }
 static int vector_f32(PyObject *t, const char *what, int device, int len, const float **out) {
     operand o;
     *out = NULL;
     if (t == Py_None) return 0;
-    if (operand_of(t, what, device, 1, &o)) return -1;
+    if (operand_of(t, what, device, 1 << 1, &o)) return -1;
     if (o.kind != MUXQ_OUT_F32 || o.cols != len) return refuse(what, "an fp32 vector of the rows' length is wanted");
     *out = o.ptr;
     return 0;
@@ -260,7 +290,7 @@ static PyObject *residual_norm(PyObject *self, PyObject *const *a, Py_ssize_t n)
     int device, group;
     if (current_place(&device, &s)) return NULL;
     if (a[0] == Py_None && a[1] == Py_None) return refuse("R", "R or Y is wanted"), NULL;
-    if (operand_of(a[0] != Py_None ? a[0] : a[1], "R", device, 2, &r)) return NULL;
+    if (operand_of(a[0] != Py_None ? a[0] : a[1], "R", device, 1 << 2, &r)) return NULL;
     const int M = r.rows, D = r.cols;
     if (a[0] == Py_None) r.ptr = NULL;
     if ((a[1] != Py_None && matrix_of(a[1], "Y", device, M, D, &y)) || (a[7] != Py_None && matrix_of(a[7], "H", device, M, D, &h)) ||
@@ -270,7 +300,7 @@ static PyObject *residual_norm(PyObject *self, PyObject *const *a, Py_ssize_t n)
     if (a[7] != Py_None && a[0] != Py_None && h.kind != r.kind) return refuse("H", "the type of R is wanted"), NULL;
     if (a[8] != Py_None && x.kind != MUXQ_OUT_F16) return refuse("X", "fp16 is wanted"), NULL;
     if (a[4] != Py_None) {
-        if (operand_of(a[4], "gate", device, 3, &g)) return NULL;
+        if (operand_of(a[4], "gate", device, 1 << 1 | 1 << 2, &g)) return NULL;
         if (group < 1) return refuse("gate_group", "at least 1 is wanted"), NULL;
         if (g.dim == 1) group = 0;
         if (g.cols != D || (g.dim == 2 && g.rows != (int)(((long long)M + group - 1) / group)))
@@ -287,41 +317,25 @@ static PyObject *residual_norm(PyObject *self, PyObject *const *a, Py_ssize_t n)
 }
 
 /* a 3-D fp16 tensor: [n][rows, cols] */
-static int stack_of(PyObject *t, const char *what, int device, void **ptr, int *n, int *rows, int *cols, int *ld, int64_t *stride) {
-    int at = -1, f16;
-    if (as_int(PyObject_CallMethodNoArgs(t, n_get_device), &at)) return -1;
-    if (at < 0) return refuse(what, "a CUDA tensor is wanted");
-    if (at != device) return refuse(what, "the tensor is on another device than the current one");
-    if ((f16 = has_dtype(t, dt_f16)) < 0) return -1;
-    if (!f16) return refuse(what, "fp16 is wanted");
-    PyObject *shape = PyObject_GetAttr(t, n_shape), *st = shape ? PyObject_CallMethodNoArgs(t, n_stride) : NULL;
-    int rc = shape && st ? 0 : -1, last = 1;
-    if (!rc && (!PyTuple_Check(shape) || PyTuple_GET_SIZE(shape) != 3 || !PyTuple_Check(st) || PyTuple_GET_SIZE(st) != 3))
-        rc = refuse(what, "three dimensions are wanted");
-    if (!rc) {
-        rc = as_int(Py_NewRef(PyTuple_GET_ITEM(shape, 0)), n) || as_int(Py_NewRef(PyTuple_GET_ITEM(shape, 1)), rows) ||
-                     as_int(Py_NewRef(PyTuple_GET_ITEM(shape, 2)), cols) || as_int(Py_NewRef(PyTuple_GET_ITEM(st, 1)), ld) ||
-                     as_int(Py_NewRef(PyTuple_GET_ITEM(st, 2)), &last)
-                 ? -1
-                 : 0;
-        *stride = PyLong_AsLongLong(PyTuple_GET_ITEM(st, 0));
-        if (PyErr_Occurred()) rc = -1;
-        if (!rc && *cols > 1 && last != 1) rc = refuse(what, "unit stride along the last dimension is wanted");
-        if (!rc && *rows == 1) *ld = *cols;
-    }
-    Py_XDECREF(shape);
-    Py_XDECREF(st);
-    return rc ? -1 : tensor_ptr(t, ptr);
+static int stack_of(PyObject *t, const char *what, int device, const void **ptr, int *n, int *rows, int *cols, int *ld, int64_t *stride) {
+    tensor_info v = {0};
+    if (cuda_info(t, what, device, 1 << 3, &v)) return -1;
+    if (v.dtype != TENSOR_F16) return refuse(what, "fp16 is wanted");
+    *ptr = v.ptr;
+    *n = (int)v.size[0];
+    *rows = (int)v.size[1];
+    *cols = (int)v.size[2];
+    *stride = v.stride[0];
+    return pitch_of(&v, 1, what, ld);
 }
 static int vector_i32(PyObject *t, const char *what, int device, int len, const int32_t **out) { /* len < 0: at least one entry */
-    int at = -1, ok, n, second, dim, sa, sb;
+    tensor_info v = {0};
     *out = NULL;
     if (t == Py_None) return 0;
-    if (as_int(PyObject_CallMethodNoArgs(t, n_get_device), &at)) return -1;
-    if (at != device) return refuse(what, at < 0 ? "a CUDA tensor is wanted" : "the tensor is on another device than the current one");
-    if ((ok = has_dtype(t, dt_i32)) < 0 || shape_of(t, &n, &second, &dim) || stride_of(t, &sa, &sb)) return -1;
-    if (!ok || dim != 1 || (n > 1 && sa != 1) || (len < 0 ? n < 1 : n != len)) return refuse(what, "a contiguous int32 vector is wanted, one entry for each row or slot");
-    return tensor_ptr(t, (void **)out);
+    if (cuda_info(t, what, device, 1 << 1, &v)) return -1;
+    if (v.dtype != TENSOR_I32 || (len < 0 ? v.size[0] < 1 : v.size[0] != len)) return refuse(what, "an int32 vector is wanted, one entry for each row or slot");
+    *out = v.ptr;
+    return 0;
 }
 
 /* adapters(X, A, B, row_slot, scale or None, rank or None, base or None, Y, status) -> status code */
@@ -329,12 +343,12 @@ static PyObject *adapters(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     if (n != 9) return PyErr_Format(PyExc_TypeError, "adapters takes 9 arguments");
     operand x = {0}, b = {0}, y = {0};
     muxq_adapter_set set = {0};
-    void *s, *pa, *pb;
+    void *s;
     const int32_t *row_slot, *status;
     int device, K, N, slots, rank;
-    if (current_place(&device, &s) || operand_of(a[0], "X", device, 2, &x) ||
-        stack_of(a[1], "A", device, &pa, &set.slots, &set.max_rank, &K, &set.lda, &set.stride_a) ||
-        stack_of(a[2], "B", device, &pb, &slots, &N, &rank, &set.ldb, &set.stride_b))
+    if (current_place(&device, &s) || operand_of(a[0], "X", device, 1 << 2, &x) ||
+        stack_of(a[1], "A", device, &set.A_f16, &set.slots, &set.max_rank, &K, &set.lda, &set.stride_a) ||
+        stack_of(a[2], "B", device, &set.B_f16, &slots, &N, &rank, &set.ldb, &set.stride_b))
         return NULL;
     if (x.kind != MUXQ_OUT_F16) return refuse("X", "fp16 is wanted"), NULL;
     if (x.cols != K) return refuse("A", "the shape does not fit X"), NULL;
@@ -344,8 +358,6 @@ static PyObject *adapters(PyObject *self, PyObject *const *a, Py_ssize_t n) {
         vector_i32(a[5], "rank", device, slots, &set.rank) || vector_i32(a[8], "status", device, -1, &status))
         return NULL;
     if (a[6] != Py_None && b.kind != y.kind) return refuse("base", "the type of Y is wanted"), NULL;
-    set.A_f16 = pa;
-    set.B_f16 = pb;
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = f_adapters(x.ptr, x.rows, K, x.ld, &set, row_slot, N, b.ptr, b.ld, y.ptr, y.ld, y.kind, (int32_t *)status, s);

@@ -182,7 +182,7 @@ def test_the_binding_refuses_what_does_not_fit(calls, mx):
                 (F((5, 8, 64)), Y, n, None, None, 1, 1.0, R, X), (F((64,)), Y, n, None, None, 1, 1.0, R, X), (R, Y, (1, 2), None, None, 1, 1.0, R, X)]:
         with pytest.raises(ValueError):
             f(*bad)
-    with pytest.raises(IndexError):
+    with pytest.raises(ValueError):
         f(F(()), Y, n, None, None, 1, 1.0, R, X)
     assert not seen
 
