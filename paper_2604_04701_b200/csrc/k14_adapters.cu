@@ -21,26 +21,25 @@ namespace {
 using namespace adapters;
 
 constexpr int kT = 256, kWarps = kT / 32;
-constexpr int kMostRows = 64;  // of a window
+constexpr int kMostRows = 32;  // of a window: a warp puts them in order
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
+__device__ __forceinline__ void st_cluster_f4(uint32_t addr, const float4 &v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 
 // Rows of T parts (fp32) and of T itself (per four ranks: four upper halves, four lower halves); the pitches keep the eight rows of
 // a fragment on different banks.
 template <int NR> __host__ __device__ constexpr int part_pitch() { return NR * 8 + 8; }                              // floats
 template <int NR> __host__ __device__ constexpr int t_pitch() { return (NR * 32 / 64 | 1) * 64; }                    // bytes
-template <int NR> __host__ __device__ constexpr size_t smem_bytes(int W) {
-    const int rows = W * kWarps < 128 ? W * kWarps : 128;  // (see k_adapters: slices of K times rows)
-    return (size_t)rows * part_pitch<NR>() * 4 + (size_t)W * t_pitch<NR>();
+template <int NR> __host__ __device__ constexpr int part_rows(int W) { return W * kWarps < 128 ? W * kWarps : 128; }  // slices of K times rows
+template <int NR> __host__ __device__ constexpr size_t smem_bytes(int W, int C) {  // parts of all CTAs, then this one's own, which T replaces
+    const size_t own = (size_t)part_rows<NR>(W) * part_pitch<NR>() * 4, t = (size_t)W * t_pitch<NR>();
+    return (size_t)C * W * part_pitch<NR>() * 4 + (own > t ? own : t);
 }
 
 // eight neighbouring results
@@ -83,11 +82,43 @@ struct Tiles {  // a window's rows in order of their adapters
     int row[kMostRows];      // by position: row within the window
     int slot[kMostRows];     // by position; rows without an adapter come last
     float factor[kMostRows]; // by position: what T B^T is multiplied by
-    int rank_of[kMostRows];  // by position
-    int key[kMostRows];      // by row: its adapter, INT_MAX without one
-    bool start[kMostRows];   // by row: the first of a tile
-    int pos[kMostRows], count[kMostRows], rank[kMostRows];  // by tile: first position, rows (up to 16), rank
+    int pos[kMostRows], count[kMostRows];  // by tile: first position, rows (up to 16)
+    int tiles, active;       // positions with an adapter
 };
+
+// Puts the rows of a window in order: one adapter's behind one another, tiles of up to 16 of them.  Called by a whole warp, lane = row.
+__device__ __forceinline__ void order_rows(Tiles *s, int key, int rows) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t valid = rows == 32 ? 0xffffffffu : (1u << rows) - 1u, below = (1u << lane) - 1u;
+    const uint32_t peers = __match_any_sync(0xffffffffu, key) & valid;
+    const bool with = key != INT_MAX;
+    const int same = __popc(peers & below), of_key = __popc(peers);
+    // in the order of the adapters' first rows: positions and tiles before each of them, in one sum
+    const uint32_t mine = with && !same ? (uint32_t)of_key | (uint32_t)((of_key + 15) >> 4) << 16 : 0u;
+    uint32_t sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += v;
+    }
+    const uint32_t total = __shfl_sync(0xffffffffu, sum, 31), before = __shfl_sync(0xffffffffu, sum - mine, peers ? __ffs(peers) - 1 : 0);
+    const int active = total & 0xffff;
+    const uint32_t without = __ballot_sync(0xffffffffu, !with) & valid;
+    if (lane < rows) {
+        const int at = with ? (int)(before & 0xffff) + same : active + __popc(without & below);
+        s->row[at] = lane;
+        s->slot[at] = with ? key : -1;
+        if (with && same % 16 == 0) {
+            const int i = (int)(before >> 16) + same / 16;
+            s->pos[i] = at;
+            s->count[i] = min(16, of_key - same);
+        }
+    }
+    if (lane == 0) {
+        s->tiles = total >> 16;
+        s->active = active;
+    }
+}
 
 template <int NR, typename TO>
 __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterArgs a, int W, int C, int behind_tiles) {
@@ -99,8 +130,8 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
     constexpr int kLane = kWide ? 8 : 4;
     using Eight = typename EightOf<TO>::type;
     using BWord = typename BWordOf<kWide>::type;
-    float *part = reinterpret_cast<float *>(smem);
-    uint8_t *tsm = smem + smem_bytes<NR>(W) - (size_t)W * kTP;
+    float *all = reinterpret_cast<float *>(smem), *part = all + (size_t)C * W * kPP;
+    uint8_t *tsm = reinterpret_cast<uint8_t *>(part);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int cta = C > 1 ? (int)cluster_ctarank() : 0;
     const int m0 = (int)(blockIdx.x / C) * W, rows = min(W, a.M - m0);
@@ -120,49 +151,34 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // behind the wait: a layer kernel may read its W_q at once
     }
 
-    // ---- rows in order of their adapters, and tiles of up to 16 rows of one adapter
-    int key = INT_MAX, rank = 0;
-    if (tid < rows) {
-        bool bad;
-        key = adapter_of(a.row_slot[m0 + tid], a.rank, a.slots, a.max_rank, &rank, &bad);
-        if (bad && cta == 0) atomicMax(a.dev_status, MUXQ_ERR_INVALID_ARG);
-        s.key[tid] = key;
-    }
-    const int active = __syncthreads_count(key != INT_MAX);
-    int at = 0, same = 0, of_key = 0;
-    if (tid < rows) {
-        int before = 0;
-        for (int j = 0; j < rows; ++j) {
-            const int k = s.key[j];
-            before += k < key;
-            same += k == key && j < tid;
-            of_key += k == key;
+    if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // waited for before anything is sent
+
+    // ---- rows in order of their adapters
+    if (warp == 0) {
+        int key = INT_MAX;
+        if (lane < rows) {
+            const int slot = a.row_slot[m0 + lane];
+            if (slot >= 0 && slot < a.slots) key = slot;
+            else if (slot != -1 && cta == 0) atomicMax(a.dev_status, MUXQ_ERR_INVALID_ARG);
         }
-        at = before + same;
-        s.row[at] = tid;
-        s.slot[at] = key == INT_MAX ? -1 : key;
-        s.rank_of[at] = rank;
-    }
-    const bool start = key != INT_MAX && same % 16 == 0;
-    if (tid < rows) s.start[tid] = start;
-    const int tiles = __syncthreads_count(start);
-    if (start) {
-        int i = same / 16;
-        for (int j = 0; j < rows; ++j) i += s.start[j] && s.key[j] < key;
-        s.pos[i] = at;
-        s.count[i] = min(16, of_key - same);
-        s.rank[i] = rank;
+        order_rows(&s, key, rows);
     }
     __syncthreads();
+    const int tiles = s.tiles, active = s.active;
+    // An adapter's rank; 0, which adds nothing, where it is out of range.
+    auto rank_of = [&](int slot) {
+        const int r = a.rank ? a.rank[slot] : a.max_rank;
+        return r < 0 || r > a.max_rank ? 0 : r;
+    };
 
     // ---- T = X A^T: this CTA's part of K.  With fewer tiles than warps the warps divide it further.
     int lanes_t = 1;  // warps side by side on different tiles: tiles rounded up to a power of two, at most all
     while (lanes_t < kWarps && lanes_t < tiles) lanes_t *= 2;
-    const int slices = kWarps / lanes_t, wt = warp & (lanes_t - 1), wk = warp / lanes_t;
-    {
-        const int chunks = (a.K + 31) >> 5, c0 = (int)((long long)chunks * cta / C), c1 = (int)((long long)chunks * (cta + 1) / C);
+    const int k_chunks = (a.K + 31) >> 5, c0 = (int)((long long)k_chunks * cta / C), c1 = (int)((long long)k_chunks * (cta + 1) / C);
+    const int slices = max(1, min(kWarps / lanes_t, c1 - c0)), wt = warp & (lanes_t - 1), wk = warp / lanes_t;
+    if (wk < slices) {
         for (int i = wt; i < tiles; i += lanes_t) {
-            const int p0 = s.pos[i], n = s.count[i], r = s.rank[i];
+            const int p0 = s.pos[i], n = s.count[i];
             float acc[NR][4];
 #pragma unroll
             for (int j = 0; j < NR; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
@@ -183,6 +199,9 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
                 }
             };
             load_x(c0 + wk);
+            // Rows of A beyond the rank are in memory and their products are not used: where there are at most 16, nothing waits for the
+            // rank; beyond that what need not be read is worth the wait.
+            const int r = NR <= 2 ? a.max_rank : rank_of(s.slot[p0]);
             for (int c = c0 + wk; c < c1; c += kAhead * slices) {
                 uint4 xu[kAhead], xv[kAhead];
 #pragma unroll
@@ -198,7 +217,7 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
                     const bool in = cc * 32 + 8 * t < a.K;
                     uint4 w[NR];
 #pragma unroll
-                    for (int j = 0; j < NR; ++j) w[j] = in && j * 8 + g < r ? *reinterpret_cast<const uint4 *>(A + (size_t)j * 8 * a.lda + cc * 32) : z;
+                    for (int j = 0; j < NR; ++j) w[j] = in && j * 8 < r ? *reinterpret_cast<const uint4 *>(A + (size_t)j * 8 * a.lda + cc * 32) : z;
 #pragma unroll
                     for (int j = 0; j < NR; ++j) {
                         if (j * 8 < r) {
@@ -219,17 +238,6 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
         }
     }
     __syncthreads();
-    if (slices > 1) {
-        for (int i = tid; i < active * NR * 8; i += kT) {
-            const int p = i / (NR * 8), r = i - p * (NR * 8);
-            if (r < s.rank_of[p]) {
-                float v = part[p * kPP + r];
-                for (int k = 1; k < slices; ++k) v += part[(k * active + p) * kPP + r];
-                part[p * kPP + r] = v;
-            }
-        }
-        if (C == 1) __syncthreads();
-    }
 
     // ---- what the second product reads beside T: on its way before T is there
     const int chunks = (a.N + 31) >> 5, q0 = (int)((long long)chunks * cta / C), q1 = (int)((long long)chunks * (cta + 1) / C);
@@ -238,9 +246,11 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
     TO *Y = static_cast<TO *>(a.Y);
     const Eight none{};
     BWord bw[kWide ? NR / 4 : 1][4];
+    int b_rank = 0;  // of the adapter whose B this is
     Eight next0 = none, next1 = none;
     auto load_b = [&](int i, int q) {
-        const int r = s.rank[i];
+        const int r = rank_of(s.slot[s.pos[i]]);
+        b_rank = r;
         const __half *B = a.B + (size_t)s.slot[s.pos[i]] * a.stride_b + kLane * t;
 #pragma unroll
         for (int k = 0; k < (kWide ? NR / 4 : 1); ++k) {
@@ -249,10 +259,19 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
             for (int j = 0; j < 4; ++j) {
                 const int col = q * 32 + (g >> 1) * 8 + 2 * j + (g & 1);
                 BWord w{};
-                if (col < a.N && k0 < r) w = *reinterpret_cast<const BWord *>(B + (size_t)col * a.ldb + 4 * kLane * k);
-                if (k0 + kLane > r) mask_beyond(w, r - k0);  // ranks beyond this adapter's own are not looked at
+                if (col < a.N && k0 < (NR <= 2 ? a.max_rank : r)) w = *reinterpret_cast<const BWord *>(B + (size_t)col * a.ldb + 4 * kLane * k);
                 bw[k][j] = w;
             }
+        }
+    };
+    auto mask_b = [&]() {  // ranks beyond the adapter's own are not looked at
+        if (NR <= 2 ? b_rank == a.max_rank : b_rank % kLane == 0) return;
+#pragma unroll
+        for (int k = 0; k < (kWide ? NR / 4 : 1); ++k) {
+            const int k0 = 4 * kLane * k + kLane * t;
+            if (k0 + kLane > b_rank)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mask_beyond(bw[k][j], b_rank - k0);
         }
     };
     auto load_base = [&](int it) {
@@ -265,24 +284,40 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
         load_b(0, q0 + warp);
         load_base(0);
     }
+    // ---- this CTA's part of T to every CTA of the cluster
+    if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // they have all started
+    for (int i = tid; i < active * NR * 2; i += kT) {
+        const int p = i / (NR * 2), r = (i - p * (NR * 2)) * 4;
+        float4 v = *reinterpret_cast<const float4 *>(part + p * kPP + r);
+        for (int k = 1; k < slices; ++k) {
+            const float4 w = *reinterpret_cast<const float4 *>(part + (k * active + p) * kPP + r);
+            v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
+        }
+        float *to = all + (size_t)(cta * W + p) * kPP + r;
+        if (C == 1) {
+            *reinterpret_cast<float4 *>(to) = v;
+        } else {
+            const uint32_t at = smem_u32(to);
+#pragma unroll 8
+            for (int c = 0; c < C; ++c) st_cluster_f4(map_to_cta(at, c), v);
+        }
+    }
     if (C > 1) cluster_sync_all();
+    else __syncthreads();
 
-    // ---- the whole of T: parts of the other CTAs, scaled and split
+    // ---- the whole of T, scaled and split, where this CTA's own parts were
     for (int p = warp; p < active; p += kWarps) {
         constexpr int kPer = (NR * 8 + 31) / 32;
-        const int r = s.rank_of[p];
+        const int r = rank_of(s.slot[p]);
+        const float scale = a.scale ? a.scale[s.slot[p]] : 1.0f;
         float v[kPer], most = 0.0f;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int j = lane + 32 * i;
             v[i] = 0.0f;
             if (j < r) {
-                if (C == 1) {
-                    v[i] = part[p * kPP + j];
-                } else {
-                    const uint32_t from = smem_u32(part + p * kPP + j);
-                    for (int c = 0; c < C; ++c) v[i] += ld_cluster_f32(map_to_cta(from, c));
-                }
+#pragma unroll 8
+                for (int c = 0; c < C; ++c) v[i] += all[(size_t)(c * W + p) * kPP + j];
             }
             most = fmaxf(most, fabsf(v[i]));
         }
@@ -302,17 +337,17 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
                 *reinterpret_cast<__half *>(to + at + (kWide ? NR * 16 : 8)) = lo;
             }
         }
-        if (lane == 0) s.factor[p] = (a.scale ? a.scale[s.slot[p]] : 1.0f) * down;
+        if (lane == 0) s.factor[p] = r ? scale * down : -0.0f;  // (-0 x 0 leaves every base as it is, -0 too)
     }
     __syncthreads();
-    // every CTA has read the others' parts behind this point: waited for at the end
-    if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 
     // ---- Y = base + T B^T: this CTA's part of N.  A warp takes 32 columns through all tiles: B stays in registers from a tile to the
     // next of the same adapter, base comes one tile ahead.
     for (int it = 0; it < items; ++it) {
-        const int i = it % tiles, p0 = s.pos[i], n = s.count[i], r = s.rank[i], q = q0 + warp + kWarps * (it / tiles);
+        const int i = it % tiles, p0 = s.pos[i], n = s.count[i], q = q0 + warp + kWarps * (it / tiles);
         if (it && (i == 0 || s.slot[p0] != s.slot[s.pos[i - 1]])) load_b(i, q);
+        if (!it || i == 0 || s.slot[p0] != s.slot[s.pos[i - 1]]) mask_b();
+        [[maybe_unused]] const int r = b_rank;
         const Eight b0 = next0, b1 = next1;
         if (it + 1 < items) load_base(it + 1);
         const int n0 = q * 32 + 8 * t;
@@ -359,10 +394,17 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
                 *reinterpret_cast<Eight *>(Y + r * a.ldy + c * 8) = base ? *reinterpret_cast<const Eight *>(base + r * a.ldbase + c * 8) : none;
         }
     }
-    __syncwarp();
+    // ---- a rank out of range is reported by the first CTA
+    if (cta == 0 && a.rank && tid < active) {
+        const int r = a.rank[s.slot[tid]];
+        if (r < 0 || r > a.max_rank) atomicMax(a.dev_status, MUXQ_ERR_INVALID_ARG);
+    }
     if (behind_tiles) asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+
+constexpr int kSmemMost = 160 * 1024;
+static_assert(smem_bytes<2>(32, 8) <= kSmemMost && smem_bytes<4>(32, 8) <= kSmemMost && smem_bytes<8>(32, 8) <= kSmemMost && smem_bytes<16>(16, 8) <= kSmemMost &&
+                  smem_bytes<16>(32, 4) <= kSmemMost, "shared memory");
 
 template <int NR, typename TO>
 cudaError_t launch_form(const AdapterArgs &a, int W, int C, bool behind_tiles, cudaStream_t s) {
@@ -373,7 +415,7 @@ cudaError_t launch_form(const AdapterArgs &a, int W, int C, bool behind_tiles, c
         std::lock_guard<std::mutex> lock(device_mutex());
         if (!done.have[dev]) {
             const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(k_adapters<NR, TO>), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                       (int)smem_bytes<NR>(kMostRows));
+                                                       kSmemMost);
             if (e != cudaSuccess) return e;
             done.have[dev] = true;
         }
@@ -381,7 +423,7 @@ cudaError_t launch_form(const AdapterArgs &a, int W, int C, bool behind_tiles, c
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)((((long long)a.M + W - 1) / W) * C));
     cfg.blockDim = dim3(kT);
-    cfg.dynamicSmemBytes = smem_bytes<NR>(W);
+    cfg.dynamicSmemBytes = smem_bytes<NR>(W, C);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -407,6 +449,7 @@ void choose(const AdapterArgs &a, int sms, int *W, int *C) {
     while (w < kMostRows && ((long long)a.M + w - 1) / w * 8 > 2 * sms) w *= 2;
     int c = 8;
     while (c > 1 && ((long long)a.M + w - 1) / w * c > 2 * sms) c /= 2;
+    if (a.max_rank > 64 && w == kMostRows && c == 8) c = 4;  // (the parts of 8 CTAs would not fit)
     *W = w;
     *C = c;
 }
