@@ -81,7 +81,8 @@ template <> struct EightOf<float> { using type = Eight32; };
 struct Tiles {  // a window's rows in order of their adapters
     int row[kMostRows];      // by position: row within the window
     int slot[kMostRows];     // by position; rows without an adapter come last
-    float factor[kMostRows]; // by position: what T B^T is multiplied by
+    int rank[kMostRows];     // by position: its adapter's rank, 0, which adds nothing, where it is out of range
+    float scale[kMostRows], factor[kMostRows]; // by position: its adapter's scale; what T B^T is multiplied by
     int pos[kMostRows], count[kMostRows];  // by tile: first position, rows (up to 16)
     int tiles, active;       // positions with an adapter
 };
@@ -121,7 +122,7 @@ __device__ __forceinline__ void order_rows(Tiles *s, int key, int rows) {
 }
 
 template <int NR, typename TO>
-__global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterArgs a, int W, int C, int behind_tiles) {
+__global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterArgs a, int W, int log_c, int behind_tiles) {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ Tiles s;
     constexpr int kPP = part_pitch<NR>(), kTP = t_pitch<NR>();
@@ -130,11 +131,12 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
     constexpr int kLane = kWide ? 8 : 4;
     using Eight = typename EightOf<TO>::type;
     using BWord = typename BWordOf<kWide>::type;
+    const int C = 1 << log_c;
     float *all = reinterpret_cast<float *>(smem), *part = all + (size_t)C * W * kPP;
     uint8_t *tsm = reinterpret_cast<uint8_t *>(part);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int cta = C > 1 ? (int)cluster_ctarank() : 0;
-    const int m0 = (int)(blockIdx.x / C) * W, rows = min(W, a.M - m0);
+    const int m0 = (int)(blockIdx.x >> log_c) * W, rows = min(W, a.M - m0);
     if (behind_tiles) {
         // k_adapter_tiles lets this kernel start behind its own wait, so what both read is there.  It has done this window, or its
         // rows are not touched by it; either way this kernel must not end before that one has.
@@ -165,16 +167,19 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
     }
     __syncthreads();
     const int tiles = s.tiles, active = s.active;
-    // An adapter's rank; 0, which adds nothing, where it is out of range.
-    auto rank_of = [&](int slot) {
-        const int r = a.rank ? a.rank[slot] : a.max_rank;
-        return r < 0 || r > a.max_rank ? 0 : r;
-    };
+    // ranks and scales are on their way beside the first operands
+    int my_rank = 0;
+    float my_scale = 1.0f;
+    if (tid < active) {
+        const int slot = s.slot[tid];
+        my_rank = a.rank ? a.rank[slot] : a.max_rank;
+        if (a.scale) my_scale = a.scale[slot];
+    }
 
     // ---- T = X A^T: this CTA's part of K.  With fewer tiles than warps the warps divide it further.
     int lanes_t = 1;  // warps side by side on different tiles: tiles rounded up to a power of two, at most all
     while (lanes_t < kWarps && lanes_t < tiles) lanes_t *= 2;
-    const int k_chunks = (a.K + 31) >> 5, c0 = (int)((long long)k_chunks * cta / C), c1 = (int)((long long)k_chunks * (cta + 1) / C);
+    const int k_chunks = (a.K + 31) >> 5, c0 = k_chunks * cta >> log_c, c1 = k_chunks * (cta + 1) >> log_c;
     const int slices = max(1, min(kWarps / lanes_t, c1 - c0)), wt = warp & (lanes_t - 1), wk = warp / lanes_t;
     if (wk < slices) {
         for (int i = wt; i < tiles; i += lanes_t) {
@@ -201,7 +206,7 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
             load_x(c0 + wk);
             // Rows of A beyond the rank are in memory and their products are not used: where there are at most 16, nothing waits for the
             // rank; beyond that what need not be read is worth the wait.
-            const int r = NR <= 2 ? a.max_rank : rank_of(s.slot[p0]);
+            const int r = NR <= 2 ? a.max_rank : min(a.rank ? a.rank[s.slot[p0]] : a.max_rank, a.max_rank);
             for (int c = c0 + wk; c < c1; c += kAhead * slices) {
                 uint4 xu[kAhead], xv[kAhead];
 #pragma unroll
@@ -237,11 +242,17 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
             }
         }
     }
+    if (tid < active) {
+        const bool bad = my_rank < 0 || my_rank > a.max_rank;
+        if (bad && cta == 0) atomicMax(a.dev_status, MUXQ_ERR_INVALID_ARG);
+        s.rank[tid] = bad ? 0 : my_rank;
+        s.scale[tid] = my_scale;
+    }
     __syncthreads();
 
     // ---- what the second product reads beside T: on its way before T is there
-    const int chunks = (a.N + 31) >> 5, q0 = (int)((long long)chunks * cta / C), q1 = (int)((long long)chunks * (cta + 1) / C);
-    const int items = tiles * (q1 - q0 > warp ? (q1 - q0 - warp + kWarps - 1) / kWarps : 0);
+    const int chunks = (a.N + 31) >> 5, q0 = chunks * cta >> log_c, q1 = chunks * (cta + 1) >> log_c;
+    const int rounds = q1 - q0 > warp ? (q1 - q0 - warp + kWarps - 1) / kWarps : 0;  // this warp's steps of 32 columns
     const TO *base = static_cast<const TO *>(a.base);
     TO *Y = static_cast<TO *>(a.Y);
     const Eight none{};
@@ -249,9 +260,9 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
     int b_rank = 0;  // of the adapter whose B this is
     Eight next0 = none, next1 = none;
     auto load_b = [&](int i, int q) {
-        const int r = rank_of(s.slot[s.pos[i]]);
+        const int p0 = s.pos[i], r = s.rank[p0];
         b_rank = r;
-        const __half *B = a.B + (size_t)s.slot[s.pos[i]] * a.stride_b + kLane * t;
+        const __half *B = a.B + (size_t)s.slot[p0] * a.stride_b + kLane * t;
 #pragma unroll
         for (int k = 0; k < (kWide ? NR / 4 : 1); ++k) {
             const int k0 = 4 * kLane * k + kLane * t;  // this lane's first rank
@@ -274,15 +285,15 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
                 for (int j = 0; j < 4; ++j) mask_beyond(bw[k][j], b_rank - k0);
         }
     };
-    auto load_base = [&](int it) {
-        const int i = it % tiles, p0 = s.pos[i], n = s.count[i], n0 = (q0 + warp + kWarps * (it / tiles)) * 32 + 8 * t;
+    auto load_base = [&](int i, int q) {
+        const int p0 = s.pos[i], n = s.count[i], n0 = q * 32 + 8 * t;
         const bool in = base && n0 < a.N;
         next0 = in && g < n ? *reinterpret_cast<const Eight *>(base + (size_t)(m0 + s.row[p0 + g]) * a.ldbase + n0) : none;
         next1 = in && g + 8 < n ? *reinterpret_cast<const Eight *>(base + (size_t)(m0 + s.row[p0 + g + 8]) * a.ldbase + n0) : none;
     };
-    if (items) {
+    if (rounds && tiles) {
         load_b(0, q0 + warp);
-        load_base(0);
+        load_base(0, q0 + warp);
     }
     // ---- this CTA's part of T to every CTA of the cluster
     if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // they have all started
@@ -308,8 +319,7 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
     // ---- the whole of T, scaled and split, where this CTA's own parts were
     for (int p = warp; p < active; p += kWarps) {
         constexpr int kPer = (NR * 8 + 31) / 32;
-        const int r = rank_of(s.slot[p]);
-        const float scale = a.scale ? a.scale[s.slot[p]] : 1.0f;
+        const int r = s.rank[p];
         float v[kPer], most = 0.0f;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
@@ -337,19 +347,24 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
                 *reinterpret_cast<__half *>(to + at + (kWide ? NR * 16 : 8)) = lo;
             }
         }
-        if (lane == 0) s.factor[p] = r ? scale * down : -0.0f;  // (-0 x 0 leaves every base as it is, -0 too)
+        if (lane == 0) s.factor[p] = r ? s.scale[p] * down : -0.0f;  // (-0 x 0 leaves every base as it is, -0 too)
     }
     __syncthreads();
 
     // ---- Y = base + T B^T: this CTA's part of N.  A warp takes 32 columns through all tiles: B stays in registers from a tile to the
     // next of the same adapter, base comes one tile ahead.
-    for (int it = 0; it < items; ++it) {
-        const int i = it % tiles, p0 = s.pos[i], n = s.count[i], q = q0 + warp + kWarps * (it / tiles);
-        if (it && (i == 0 || s.slot[p0] != s.slot[s.pos[i - 1]])) load_b(i, q);
-        if (!it || i == 0 || s.slot[p0] != s.slot[s.pos[i - 1]]) mask_b();
+    for (int i = 0, q = q0 + warp, fresh = 1, left = rounds * tiles; left > 0; --left) {
+        const int p0 = s.pos[i], n = s.count[i];
+        if (!fresh && (i == 0 || s.slot[p0] != s.slot[s.pos[i - 1]])) {
+            load_b(i, q);
+            fresh = 1;
+        }
+        if (fresh) mask_b();
+        fresh = 0;
         [[maybe_unused]] const int r = b_rank;
         const Eight b0 = next0, b1 = next1;
-        if (it + 1 < items) load_base(it + 1);
+        const int next_i = i + 1 < tiles ? i + 1 : 0, next_q = next_i ? q : q + kWarps;
+        if (left > 1) load_base(next_i, next_q);
         const int n0 = q * 32 + 8 * t;
         float acc[4][4];
 #pragma unroll
@@ -384,6 +399,8 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
         const float o1[8] = {acc[0][2], acc[0][3], acc[1][2], acc[1][3], acc[2][2], acc[2][3], acc[3][2], acc[3][3]};
         if (n0 < a.N && g < n) add_store(Y + (size_t)(m0 + s.row[g0]) * a.ldy + n0, b0, o0, s.factor[g0]);
         if (n0 < a.N && g + 8 < n) add_store(Y + (size_t)(m0 + s.row[g1]) * a.ldy + n0, b1, o1, s.factor[g1]);
+        i = next_i;
+        q = next_q;
     }
     // ---- rows without an adapter
     if (base != Y) {
@@ -393,11 +410,6 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
             for (int c = first + lane; c < last; c += 32)
                 *reinterpret_cast<Eight *>(Y + r * a.ldy + c * 8) = base ? *reinterpret_cast<const Eight *>(base + r * a.ldbase + c * 8) : none;
         }
-    }
-    // ---- a rank out of range is reported by the first CTA
-    if (cta == 0 && a.rank && tid < active) {
-        const int r = a.rank[s.slot[tid]];
-        if (r < 0 || r > a.max_rank) atomicMax(a.dev_status, MUXQ_ERR_INVALID_ARG);
     }
     if (behind_tiles) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
@@ -420,6 +432,8 @@ cudaError_t launch_form(const AdapterArgs &a, int W, int C, bool behind_tiles, c
             done.have[dev] = true;
         }
     }
+    int log_c = 0;
+    while (1 << log_c < C) ++log_c;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)((((long long)a.M + W - 1) / W) * C));
     cfg.blockDim = dim3(kT);
@@ -432,7 +446,7 @@ cudaError_t launch_form(const AdapterArgs &a, int W, int C, bool behind_tiles, c
     attr[1].val.clusterDim.x = C; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = C > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, k_adapters<NR, TO>, a, W, C, (int)behind_tiles);
+    return cudaLaunchKernelEx(&cfg, k_adapters<NR, TO>, a, W, log_c, (int)behind_tiles);
 }
 
 template <typename TO>

@@ -73,12 +73,15 @@ __device__ __forceinline__ void mbar_arrive_elect(uint64_t *bar) {
         : "memory");
 }
 
+// Where part i of n begins when they are as even as they come.
+__device__ __forceinline__ int part_begin(int total, int i, int n) { return total / n * i + min(i, total % n); }
+
 // A window without adapters: this CTA's columns of base.
 template <bool kF32>
 __device__ __forceinline__ void copy_window(const TileParams &p, int m0) {
     if (p.base == p.Y) return;
     constexpr int kSize = kF32 ? 4 : 2, kPer = 16 / kSize, kAhead = 4;
-    const int words = p.N / kPer, w0 = (int)((long long)words * blockIdx.y / gridDim.y), n = (int)((long long)words * (blockIdx.y + 1) / gridDim.y) - w0;
+    const int words = p.N / kPer, w0 = part_begin(words, blockIdx.y, gridDim.y), n = part_begin(words, blockIdx.y + 1, gridDim.y) - w0;
     const int total = min(128, p.M - m0) * n;
     for (int i = threadIdx.x; i < total; i += kAhead * kThreads) {
         uint4 v[kAhead];
@@ -156,7 +159,7 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
     volatile uint32_t *abort_flag = &s_abort;
     const int bufs = d <= 2 ? 4 : 2, buf_cols = 512 / bufs;  // accumulators: a step of N for every adapter
     const int chunks = (p.K + 63) >> 6, units = (p.N + kUnit - 1) / kUnit;
-    const int u0 = (int)((long long)units * blockIdx.y / gridDim.y), u1 = (int)((long long)units * (blockIdx.y + 1) / gridDim.y);
+    const int u0 = part_begin(units, blockIdx.y, gridDim.y), u1 = part_begin(units, blockIdx.y + 1, gridDim.y);
 
     if (warp == 0) {
         // ------------------------------------------------------------ X and A, then base
