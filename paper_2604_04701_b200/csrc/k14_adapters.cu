@@ -21,7 +21,8 @@ namespace {
 using namespace adapters;
 
 constexpr int kT = 256, kWarps = kT / 32;
-constexpr int kMostRows = 32;  // of a window: a warp puts them in order
+constexpr int kMostRows = 32;     // of a window: a warp puts them in order
+constexpr int kSmemMost = 220 * 1024;
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -36,7 +37,7 @@ __device__ __forceinline__ void st_cluster_f4(uint32_t addr, const float4 &v) {
 // a fragment on different banks.
 template <int NR> __host__ __device__ constexpr int part_pitch() { return NR * 8 + 8; }                              // floats
 template <int NR> __host__ __device__ constexpr int t_pitch() { return (NR * 32 / 64 | 1) * 64; }                    // bytes
-template <int NR> __host__ __device__ constexpr int part_rows(int W) { return W * kWarps < 128 ? W * kWarps : 128; }  // slices of K times rows
+template <int NR> __host__ __device__ constexpr int part_rows(int W) { return W * kWarps < 128 ? W * kWarps : 128; }  // slices of K times rows (W <= 128)
 template <int NR> __host__ __device__ constexpr size_t smem_bytes(int W, int C) {  // parts of all CTAs, then this one's own, which T replaces
     const size_t own = (size_t)part_rows<NR>(W) * part_pitch<NR>() * 4, t = (size_t)W * t_pitch<NR>();
     return (size_t)C * W * part_pitch<NR>() * 4 + (own > t ? own : t);
@@ -78,17 +79,18 @@ template <typename T> struct EightOf;
 template <> struct EightOf<__half> { using type = uint4; };
 template <> struct EightOf<float> { using type = Eight32; };
 
+template <int kRows>
 struct Tiles {  // a window's rows in order of their adapters
-    int row[kMostRows];      // by position: row within the window
-    int slot[kMostRows];     // by position; rows without an adapter come last
-    int rank[kMostRows];     // by position: its adapter's rank, 0, which adds nothing, where it is out of range
-    float scale[kMostRows], factor[kMostRows]; // by position: its adapter's scale; what T B^T is multiplied by
-    int pos[kMostRows], count[kMostRows];  // by tile: first position, rows (up to 16)
-    int tiles, active;       // positions with an adapter
+    int row[kRows];      // by position: row within the window
+    int slot[kRows];     // by position; rows without an adapter come last
+    int rank[kRows];     // by position: its adapter's rank, 0, which adds nothing, where it is out of range
+    float scale[kRows], factor[kRows]; // by position: its adapter's scale; what T B^T is multiplied by
+    int pos[kRows], count[kRows];  // by tile: first position, rows (up to 16)
+    int tiles, active;   // positions with an adapter
 };
 
 // Puts the rows of a window in order: one adapter's behind one another, tiles of up to 16 of them.  Called by a whole warp, lane = row.
-__device__ __forceinline__ void order_rows(Tiles *s, int key, int rows) {
+__device__ __forceinline__ void order_rows(Tiles<kMostRows> *s, int key, int rows) {
     const int lane = threadIdx.x & 31;
     const uint32_t valid = rows == 32 ? 0xffffffffu : (1u << rows) - 1u, below = (1u << lane) - 1u;
     const uint32_t peers = __match_any_sync(0xffffffffu, key) & valid;
@@ -121,10 +123,45 @@ __device__ __forceinline__ void order_rows(Tiles *s, int key, int rows) {
     }
 }
 
-template <int NR, typename TO>
-__global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterArgs a, int W, int log_c, int behind_tiles) {
+// The same for 128 rows, by a whole CTA: every row counts those that come before it.
+__device__ __forceinline__ void order_rows(Tiles<kWindow> *s, int key, int rows) {
+    __shared__ int keys[kWindow];
+    __shared__ bool start[kWindow];
+    const int tid = threadIdx.x;
+    if (tid < rows) keys[tid] = key;
+    const int active = __syncthreads_count(key != INT_MAX);
+    int at = 0, same = 0, of_key = 0;
+    if (tid < rows) {
+        for (int j = 0; j < rows; ++j) {
+            const int k = keys[j];
+            at += k < key || (k == key && j < tid);
+            same += k == key && j < tid;
+            of_key += k == key;
+        }
+        s->row[at] = tid;
+        s->slot[at] = key == INT_MAX ? -1 : key;
+    }
+    const bool first = key != INT_MAX && same % 16 == 0;
+    if (tid < rows) start[tid] = first;
+    const int tiles = __syncthreads_count(first);
+    if (first) {
+        int i = same / 16;
+        for (int j = 0; j < rows; ++j) i += start[j] && keys[j] < key;
+        s->pos[i] = at;
+        s->count[i] = min(16, of_key - same);
+    }
+    if (tid == 0) {
+        s->tiles = tiles;
+        s->active = active;
+    }
+}
+
+// kBehind: windows of 128 rows that k_adapter_tiles has left (k15_adapter_tiles.cu).  Larger windows have more rows of an adapter to share its
+// A and B: 12000 rows of 16 adapters in any order, 1280 -> 2560, rank 64: FIGURE.
+template <int NR, typename TO, bool kBehind>
+__global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterArgs a, int W, int log_c) {
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ Tiles s;
+    __shared__ Tiles<kBehind ? kWindow : kMostRows> s;
     constexpr int kPP = part_pitch<NR>(), kTP = t_pitch<NR>();
     // A lane of the second product holds eight neighbouring ranks of T and B (two instructions' worth), four where ranks end at 16
     constexpr bool kWide = NR >= 4;
@@ -137,14 +174,14 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int cta = C > 1 ? (int)cluster_ctarank() : 0;
     const int m0 = (int)(blockIdx.x >> log_c) * W, rows = min(W, a.M - m0);
-    if (behind_tiles) {
+    if constexpr (kBehind) {
         // k_adapter_tiles lets this kernel start behind its own wait, so what both read is there.  It has done this window, or its
         // rows are not touched by it; either way this kernel must not end before that one has.
         __shared__ WindowAdapters s_win;
         int mine;
         bool bad;
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-        if (window_adapters(&s_win, a.row_slot, a.rank, a.slots, a.max_rank, m0 / kWindow * kWindow, a.M, &mine, &bad)) {
+        if (window_adapters(&s_win, a.row_slot, a.rank, a.slots, a.max_rank, m0, a.M, &mine, &bad)) {
             asm volatile("griddepcontrol.wait;" ::: "memory");
             return;
         }
@@ -156,10 +193,10 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // waited for before anything is sent
 
     // ---- rows in order of their adapters
-    if (warp == 0) {
+    if (kBehind || warp == 0) {
         int key = INT_MAX;
-        if (lane < rows) {
-            const int slot = a.row_slot[m0 + lane];
+        if (tid < rows) {
+            const int slot = a.row_slot[m0 + tid];
             if (slot >= 0 && slot < a.slots) key = slot;
             else if (slot != -1 && cta == 0) atomicMax(a.dev_status, MUXQ_ERR_INVALID_ARG);
         }
@@ -411,61 +448,53 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
                 *reinterpret_cast<Eight *>(Y + r * a.ldy + c * 8) = base ? *reinterpret_cast<const Eight *>(base + r * a.ldbase + c * 8) : none;
         }
     }
-    if (behind_tiles) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if constexpr (kBehind) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-constexpr int kSmemMost = 160 * 1024;
 static_assert(smem_bytes<2>(32, 8) <= kSmemMost && smem_bytes<4>(32, 8) <= kSmemMost && smem_bytes<8>(32, 8) <= kSmemMost && smem_bytes<16>(16, 8) <= kSmemMost &&
-                  smem_bytes<16>(32, 4) <= kSmemMost, "shared memory");
+                  smem_bytes<16>(32, 4) <= kSmemMost && smem_bytes<16>(kWindow, 1) <= kSmemMost, "shared memory");
 
-template <int NR, typename TO>
-cudaError_t launch_form(const AdapterArgs &a, int W, int C, bool behind_tiles, cudaStream_t s) {
+template <int NR, typename TO, bool kBehind>
+cudaError_t launch_form(const AdapterArgs &a, int sms, cudaStream_t s) {
     static PerDevice<int> done;
     const int dev = current_device();
     if (dev < 0) return cudaErrorInvalidDevice;
     {
         std::lock_guard<std::mutex> lock(device_mutex());
         if (!done.have[dev]) {
-            const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(k_adapters<NR, TO>), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                       kSmemMost);
+            const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(k_adapters<NR, TO, kBehind>),
+                                                       cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost);
             if (e != cudaSuccess) return e;
             done.have[dev] = true;
         }
     }
-    int log_c = 0;
-    while (1 << log_c < C) ++log_c;
+    // As many CTAs as the device holds two of on an SM: clusters of 8 as long as windows of up to 32 rows make few enough of them, then smaller
+    // ones.  (1 x 768 -> 768 ... FIGURES)
+    const auto windows = [&](int rows) { return ((long long)a.M + rows - 1) / rows; };
+    int W = kBehind ? kWindow : 1, log_c = 3;
+    while (!kBehind && W < kMostRows && windows(W) * 8 > 2 * sms) W *= 2;
+    while (log_c && (windows(W) << log_c > 2 * sms || smem_bytes<NR>(W, 1 << log_c) > kSmemMost)) --log_c;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)((((long long)a.M + W - 1) / W) * C));
+    cfg.gridDim = dim3((unsigned)(windows(W) << log_c));
     cfg.blockDim = dim3(kT);
-    cfg.dynamicSmemBytes = smem_bytes<NR>(W, C);
+    cfg.dynamicSmemBytes = smem_bytes<NR>(W, 1 << log_c);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = C; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    attr[1].val.clusterDim.x = 1 << log_c; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = C > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, k_adapters<NR, TO>, a, W, log_c, (int)behind_tiles);
+    cfg.numAttrs = log_c ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, k_adapters<NR, TO, kBehind>, a, W, log_c);
 }
 
-template <typename TO>
-cudaError_t launch_type(const AdapterArgs &a, int W, int C, bool behind_tiles, cudaStream_t s) {
-    if (a.max_rank <= 16) return launch_form<2, TO>(a, W, C, behind_tiles, s);
-    if (a.max_rank <= 32) return launch_form<4, TO>(a, W, C, behind_tiles, s);
-    if (a.max_rank <= 64) return launch_form<8, TO>(a, W, C, behind_tiles, s);
-    return launch_form<16, TO>(a, W, C, behind_tiles, s);
-}
-
-// Rows of a window and CTAs of its cluster.
-void choose(const AdapterArgs &a, int sms, int *W, int *C) {
-    int w = 1;
-    while (w < kMostRows && ((long long)a.M + w - 1) / w * 8 > 2 * sms) w *= 2;
-    int c = 8;
-    while (c > 1 && ((long long)a.M + w - 1) / w * c > 2 * sms) c /= 2;
-    if (a.max_rank > 64 && w == kMostRows && c == 8) c = 4;  // (the parts of 8 CTAs would not fit)
-    *W = w;
-    *C = c;
+template <typename TO, bool kBehind>
+cudaError_t launch_type(const AdapterArgs &a, int sms, cudaStream_t s) {
+    if (a.max_rank <= 16) return launch_form<2, TO, kBehind>(a, sms, s);
+    if (a.max_rank <= 32) return launch_form<4, TO, kBehind>(a, sms, s);
+    if (a.max_rank <= 64) return launch_form<8, TO, kBehind>(a, sms, s);
+    return launch_form<16, TO, kBehind>(a, sms, s);
 }
 
 }  // namespace
@@ -473,12 +502,11 @@ void choose(const AdapterArgs &a, int sms, int *W, int *C) {
 cudaError_t launch_adapters(const AdapterArgs &a, cudaStream_t s) {
     const int sms = num_sms();
     if (sms < 1) return cudaErrorInvalidDevice;
-    int W, C;
-    choose(a, sms, &W, &C);
     cudaError_t e = cudaSuccess;
-    const bool behind_tiles = launch_adapter_tiles(a, s, &e);
+    const bool behind = launch_adapter_tiles(a, s, &e);
     if (e != cudaSuccess) return e;
-    return a.out_f32 ? launch_type<float>(a, W, C, behind_tiles, s) : launch_type<__half>(a, W, C, behind_tiles, s);
+    if (a.out_f32) return behind ? launch_type<float, true>(a, sms, s) : launch_type<float, false>(a, sms, s);
+    return behind ? launch_type<__half, true>(a, sms, s) : launch_type<__half, false>(a, sms, s);
 }
 
 }  // namespace muxq

@@ -14,6 +14,8 @@
 // lanes, the first group also for T), steps of N dealt out in turn so that their chains of latencies overlap; the last warp TMA for B.  Every wait is bounded; on expiry the CTA raises MUXQ_ERR_TIMEOUT, lets its copies and products end and returns.
 #include <limits.h>
 
+#include <type_traits>
+
 #include "../../include/muxq.h"
 #include "gemm_common.cuh"
 #include "k14_adapters.cuh"
@@ -28,10 +30,15 @@ constexpr int kGroups = 2;                // of four result warps; a group takes
 constexpr int kThreads = 32 * (3 + 4 * kGroups), kWarpB = 2 + 4 * kGroups;
 constexpr int kUnit = 64;                 // columns of N at a time
 constexpr int kBox = 128 * 128;           // bytes of 128 rows x 128 bytes
-constexpr int kXStages = 3, kXStage = 2 * kBox;  // X 128 x 64, then A: 128 rows of 64 at most
+constexpr int kXRing = 6 * kBox, kMaxX = 6;  // stages of X, 128 x 64, and A, up to 128 rows of 64
 constexpr int kTB = 96 * 1024;            // T (32 or 64 KB) and the ring of B
 constexpr int kMaxB = 4, kMaxBase = 8;
-constexpr int kSmem = kTB + 2 * kBox + kXStages * kXStage + 1024;  // + alignment
+constexpr int kSmem = kTB + 2 * kBox + kXRing + 1024;  // + alignment
+
+// Steps of N that one instruction of the second product covers, so that T, which it reads from shared memory every time, is read less often:
+// with one step an instruction the kernel was bound by shared memory (T and B 48 KB of 112 KB a step; 82 us at 16384 x 1280 -> 5120).  As many as
+// two accumulators for every adapter have columns for, and two stages of B room.
+__host__ __device__ constexpr int group_units(int adapters, bool high) { return high || adapters > 2 ? 1 : adapters == 2 ? 2 : 4; }
 
 struct TileParams {
     int M, K, N, slots, max_rank;
@@ -105,14 +112,22 @@ __global__ void __launch_bounds__(kThreads, 1)
 k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
                 const __grid_constant__ CUtensorMap tm_base, const __grid_constant__ CUtensorMap tm_y, const TileParams p) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t x_full[kXStages], x_empty[kXStages], b_full[kMaxB], b_empty[kMaxB], base_full[kMaxBase], base_empty[kMaxBase];
-    __shared__ uint64_t t_full, t_ready, acc_full[4], acc_empty[4], drained;
+    __shared__ uint64_t x_full[kMaxX], x_empty[kMaxX], b_full[kMaxB], b_empty[kMaxB], base_full[kMaxBase], base_empty[kMaxBase];
+    __shared__ uint64_t t_full, t_ready, acc_full[2], acc_empty[2], drained;
     __shared__ float s_factor[128];
     __shared__ WindowAdapters s_win;
     __shared__ uint32_t s_tmem, s_abort;
 
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int m0 = blockIdx.x * 128;
+    if (threadIdx.x == 0) {
+        // (the first copy by a map that is not at hand took 3300 cycles to be issued)
+        tma_prefetch_desc(&tm_x);
+        tma_prefetch_desc(&tm_a);
+        tma_prefetch_desc(&tm_b);
+        tma_prefetch_desc(&tm_base);
+        tma_prefetch_desc(&tm_y);
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // behind the wait: k_adapters may look at the rows at once
     int mine;
@@ -128,22 +143,23 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
     // shared memory: T (upper halves, lower halves) | ring of B | two boxes for base | stages of X and A, later base too
     const uint32_t base_addr = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *sm = smem_raw + (base_addr - smem_u32(smem_raw));
-    const int t_bytes = R64 * 2 * kBox, b_stage = d * R64 * (kBox / 2);
+    const int x_stage = kBox + d * R16 * 128, x_stages = min(kXRing / x_stage, kMaxX);
+    const int t_bytes = R64 * 2 * kBox, G = group_units(d, R64 == 2), b_stage = d * R64 * G * (kBox / 2);
     int b_stages = (kTB - t_bytes) / b_stage;
     if (b_stages > kMaxB) b_stages = kMaxB;
     constexpr int kBaseStage = kF32 ? 2 * kBox : kBox;
-    constexpr int kBaseStages = (2 * kBox + kXStages * kXStage) / kBaseStage;  // 8, fp32 4
+    constexpr int kBaseStages = (2 * kBox + kXRing) / kBaseStage;  // 8, fp32 4
     constexpr int kBaseEarly = 2 * kBox / kBaseStage;                          // those that do not lie over X and A
-    static_assert(kBaseStages <= kMaxBase, "ring of base");
+    static_assert(kBaseStages <= kMaxBase && kBaseStages > kGroups, "ring of base (a group gives a tile back with its next one)");
     uint8_t *sm_t = sm, *sm_b = sm + t_bytes, *sm_base = sm + kTB, *sm_x = sm_base + 2 * kBox;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kXStages; ++i) { mbar_init(&x_full[i], 1); mbar_init(&x_empty[i], 1); }
+        for (int i = 0; i < kMaxX; ++i) { mbar_init(&x_full[i], 1); mbar_init(&x_empty[i], 1); }
         for (int i = 0; i < kMaxB; ++i) { mbar_init(&b_full[i], 1); mbar_init(&b_empty[i], 1); }
         for (int i = 0; i < kMaxBase; ++i) { mbar_init(&base_full[i], 1); mbar_init(&base_empty[i], 4); }
         mbar_init(&t_full, 1);
         mbar_init(&t_ready, 4);
-        for (int i = 0; i < 4; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4 * G); }
         mbar_init(&drained, 1);
         s_abort = 0;
         fence_barrier_init();
@@ -157,7 +173,6 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
     volatile uint32_t *abort_flag = &s_abort;
-    const int bufs = d <= 2 ? 4 : 2, buf_cols = 512 / bufs;  // accumulators: a step of N for every adapter
     const int chunks = (p.K + 63) >> 6, units = (p.N + kUnit - 1) / kUnit;
     const int u0 = part_begin(units, blockIdx.y, gridDim.y), u1 = part_begin(units, blockIdx.y + 1, gridDim.y);
 
@@ -180,10 +195,10 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
         };
         for (; issued_base < kBaseEarly && issued_base < u1 - u0 && ok; ++issued_base) ok = load_base(issued_base);
         for (; issued_x < chunks && ok; ++issued_x) {
-            const int s = issued_x % kXStages;
-            if (!mbar_wait_warp(&x_empty[s], ((issued_x / kXStages) & 1) ^ 1, abort_flag, p.spin)) { ok = false; break; }
+            const int s = issued_x % x_stages;
+            if (!mbar_wait_warp(&x_empty[s], ((issued_x / x_stages) & 1) ^ 1, abort_flag, p.spin)) { ok = false; break; }
             if (issued_x == p.skip_chunk) continue;
-            uint8_t *to = sm_x + s * kXStage;
+            uint8_t *to = sm_x + s * x_stage;
             mbar_expect_tx_elect(&x_full[s], kBox + d * R8 * 128);
             tma_load_2d_elect(to, &tm_x, &x_full[s], issued_x * 64, m0);
             for (int i = 0; i < d; ++i) tma_load_3d_elect(to + kBox + i * R16 * 128, &tm_a, &x_full[s], issued_x * 64, 0, s_win.slot[i]);
@@ -193,10 +208,10 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
         for (; issued_base < u1 - u0 && ok; ++issued_base)
             if (!load_base(issued_base)) { ok = false; break; }
         if (!ok) {  // every copy that was started lands before the CTA ends
-            for (int k = issued_x > kXStages ? issued_x - kXStages : 0; k < issued_x; ++k)
+            for (int k = issued_x > x_stages ? issued_x - x_stages : 0; k < issued_x; ++k)
                 if (k != p.skip_chunk)
                     for (uint32_t i = 0; i < kSpinLimit; ++i)
-                        if (__all_sync(0xffffffffu, mbar_try_wait(&x_full[k % kXStages], (k / kXStages) & 1))) break;
+                        if (__all_sync(0xffffffffu, mbar_try_wait(&x_full[k % x_stages], (k / x_stages) & 1))) break;
             for (int k = issued_base > kBaseStages ? issued_base - kBaseStages : 0; k < issued_base; ++k)
                 for (uint32_t i = 0; i < kSpinLimit; ++i)
                     if (__all_sync(0xffffffffu, mbar_try_wait(&base_full[k % kBaseStages], (k / kBaseStages) & 1))) break;
@@ -205,13 +220,13 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
         // ------------------------------------------------------------ B
         int issued = 0;
         bool ok = true;
-        for (; issued < u1 - u0 && ok; ++issued) {
-            const int s = issued % b_stages;
+        for (; issued * G < u1 - u0 && ok; ++issued) {
+            const int s = issued % b_stages, n = min(G, u1 - u0 - issued * G);
             if (!mbar_wait_warp(&b_empty[s], ((issued / b_stages) & 1) ^ 1, abort_flag, p.spin)) { ok = false; break; }
-            mbar_expect_tx_elect(&b_full[s], b_stage);
-            for (int i = 0; i < d; ++i)
-                for (int k = 0; k < R64; ++k)
-                    tma_load_3d_elect(sm_b + s * b_stage + (i * R64 + k) * (kBox / 2), &tm_b, &b_full[s], k * 64, (u0 + issued) * kUnit, s_win.slot[i]);
+            mbar_expect_tx_elect(&b_full[s], d * R64 * n * (kBox / 2));
+            for (int i = 0; i < d * R64; ++i)
+                for (int k = 0; k < n; ++k)
+                    tma_load_3d_elect(sm_b + s * b_stage + (i * G + k) * (kBox / 2), &tm_b, &b_full[s], i % R64 * 64, (u0 + issued * G + k) * kUnit, s_win.slot[i / R64]);
         }
         if (!ok)
             for (int k = issued > b_stages ? issued - b_stages : 0; k < issued; ++k)
@@ -219,42 +234,71 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
                     if (__all_sync(0xffffffffu, mbar_try_wait(&b_full[k % b_stages], (k / b_stages) & 1))) break;
     } else if (warp == 1) {
         // ------------------------------------------------------------ products
+        // Addresses and descriptors have to be uniform to the compiler, too, or every instruction waits for several moves to uniform registers: they
+        // are made of kernel arguments, loop counters and constants, and the number of adapters, which shared memory tells, is one of the latter.
+        // All of tensor memory is ours, so it begins at 0.
         bool ok = true;
-        const uint32_t idesc_t = idesc_f16(R16), idesc_y = idesc_f16(kUnit);
-        const uint64_t x_desc = smem_desc_sw128(smem_u32(sm_x));
-        for (int c = 0; c < chunks; ++c) {
-            const int s = c % kXStages;
-            if (!mbar_wait_warp(&x_full[s], (c / kXStages) & 1, abort_flag, p.spin)) { ok = false; break; }
-            tc_fence_after();
-            const uint64_t xd = x_desc + (uint64_t)(s * (kXStage >> 4)), ad = xd + (kBox >> 4);
-            const int steps = min(4, (p.K - c * 64 + 15) >> 4);
-            for (int i = 0; i < d; ++i)
-                for (int k = 0; k < steps; ++k)
-                    mma_f16_elect(tmem + i * R16, xd + 2 * k, ad + (uint64_t)(i * R16 * 8) + 2 * k, idesc_t, c || k ? 1u : 0u);
-            mma_commit_elect(&x_empty[s]);
-        }
-        if (ok) {
-            mma_commit_elect(&t_full);
-            ok = mbar_wait_warp(&t_ready, 0, abort_flag, p.spin);
-            tc_fence_after();
-        }
-        const uint64_t t_desc = smem_desc_sw128(smem_u32(sm_t)), b_desc = smem_desc_sw128(smem_u32(sm_b));
-        for (int u = 0; u < u1 - u0 && ok; ++u) {
-            const int s = u % b_stages, buf = u % bufs;
-            if (!mbar_wait_warp(&acc_empty[buf], ((u / bufs) & 1) ^ 1, abort_flag, p.spin) ||
-                !mbar_wait_warp(&b_full[s], (u / b_stages) & 1, abort_flag, p.spin)) { ok = false; break; }
-            tc_fence_after();
-            for (int i = 0; i < d; ++i) {
-                const int steps = (s_win.rank[i] + 15) >> 4;
-                for (int half = 0; half < 2; ++half)
-                    for (int k = 0; k < steps; ++k) {
-                        const int blk = k >> 2, in = (k & 3) * 2;
-                        mma_f16_elect(tmem + buf * buf_cols + i * kUnit, t_desc + (uint64_t)((half * R64 + blk) * (kBox >> 4)) + in,
-                                      b_desc + (uint64_t)((s * b_stage + (i * R64 + blk) * (kBox / 2)) >> 4) + in, idesc_y, half || k ? 1u : 0u);
-                    }
+        const uint32_t sm0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
+        auto issue = [&](auto number) {
+            constexpr int D = decltype(number)::value;
+            const int r16 = (p.max_rank + 15) & ~15, blocks = p.max_rank > 64 ? 2 : 1;
+            const int xb = kBox + D * r16 * 128, xs = min(kXRing / xb, kMaxX);
+            const int units_g = group_units(D, blocks == 2), bb = D * blocks * units_g * (kBox / 2), bs = min((kTB - blocks * 2 * kBox) / bb, kMaxB);
+            const uint32_t idesc_t = idesc_f16(r16), idesc_y = idesc_f16(units_g * kUnit);
+            const uint64_t x_desc = smem_desc_sw128(sm0 + kTB + 2 * kBox);
+            for (int c = 0, st = 0, ph = 0; c < chunks; ++c) {
+                if (!mbar_wait_warp(&x_full[st], ph, abort_flag, p.spin)) return false;
+                tc_fence_after();
+                const uint64_t xd = x_desc + (uint64_t)(uint32_t)(st * (xb >> 4));
+                const int steps = (p.K - c * 64 + 15) >> 4;  // of 16
+#pragma unroll
+                for (int i = 0; i < D; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k < steps) mma_f16_elect(i * r16, xd + 2 * k, xd + (uint64_t)(uint32_t)((kBox >> 4) + i * r16 * 8 + 2 * k), idesc_t, k ? 1u : c ? 1u : 0u);
+                mma_commit_elect(&x_empty[st]);
+                if (++st == xs) { st = 0; ph ^= 1; }
             }
-            mma_commit_elect(&b_empty[s]);
-            mma_commit_elect(&acc_full[buf]);
+            mma_commit_elect(&t_full);
+            if (!mbar_wait_warp(&t_ready, 0, abort_flag, p.spin)) return false;
+            tc_fence_after();
+            uint32_t packed = 0;  // steps of 16 ranks of every adapter
+#pragma unroll
+            for (int i = 0; i < D; ++i) packed |= (uint32_t)((s_win.rank[i] + 15) >> 4) << (8 * i);
+            const uint64_t t_desc = smem_desc_sw128(sm0), b_desc = smem_desc_sw128(sm0 + blocks * 2 * kBox);
+            const int count = (u1 - u0 + units_g - 1) / units_g;
+            for (int u = 0, st = 0, ph = 0, buf = 0, bph = 1; u < count; ++u) {
+                if (!mbar_wait_warp(&acc_empty[buf], bph, abort_flag, p.spin) || !mbar_wait_warp(&b_full[st], ph, abort_flag, p.spin)) return false;
+                tc_fence_after();
+                auto products = [&](auto blocks_c) {
+                    constexpr int kB = decltype(blocks_c)::value, kG = group_units(D, kB == 2);  // blocks of 64 ranks
+#pragma unroll
+                    for (int i = 0; i < D; ++i) {
+                        const int steps = packed >> (8 * i) & 0xff;
+                        const uint64_t bd = b_desc + (uint64_t)(uint32_t)(st * (bb >> 4) + i * kB * kG * (kBox >> 5));
+#pragma unroll
+                        for (int half = 0; half < 2; ++half)
+#pragma unroll
+                            for (int k = 0; k < 4 * kB; ++k)
+                                if (k < steps)
+                                    mma_f16_elect(buf * 256 + i * kG * kUnit, t_desc + (uint64_t)((half * kB + (k >> 2)) * (kBox >> 4) + (k & 3) * 2),
+                                                  bd + (uint64_t)((k >> 2) * kG * (kBox >> 5) + (k & 3) * 2), idesc_y, half || k ? 1u : 0u);
+                    }
+                };
+                if (blocks == 1) products(std::integral_constant<int, 1>{});
+                else products(std::integral_constant<int, 2>{});
+                mma_commit_elect(&b_empty[st]);
+                mma_commit_elect(&acc_full[buf]);
+                if (++st == bs) { st = 0; ph ^= 1; }
+                if (++buf == 2) { buf = 0; bph ^= 1; }
+            }
+            return true;
+        };
+        switch (d) {
+            case 1: ok = issue(std::integral_constant<int, 1>{}); break;
+            case 2: ok = issue(std::integral_constant<int, 2>{}); break;
+            case 3: ok = issue(std::integral_constant<int, 3>{}); break;
+            default: ok = issue(std::integral_constant<int, 4>{}); break;
         }
         if (!ok) {  // products that are on their way end before their memory is given back
             mma_commit_elect(&drained);
@@ -317,29 +361,26 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
         }
         if (ok) ok = mbar_wait_warp(&t_ready, 0, abort_flag, p.spin);
         const float f = ok ? s_factor[row] : 0.0f;
+        const int first = present ? __ffs(present) - 1 : 0;
         int last = -1;  // tile of base whose store may still be reading it
         for (int u = group; u < u1 - u0 && ok; u += kGroups) {
-            const int s = u % kBaseStages, buf = u % bufs;
-            if (!mbar_wait_warp(&acc_full[buf], (u / bufs) & 1, abort_flag, p.spin)) { ok = false; break; }
+            const int s = u % kBaseStages, step = u / G, buf = step & 1;
+            if (!mbar_wait_warp(&acc_full[buf], (step >> 1) & 1, abort_flag, p.spin)) { ok = false; break; }
             tc_fence_after();
             uint32_t v[64];
-            const uint32_t from = taddr + buf * buf_cols;
-            if ((present & (present - 1)) == 0) {  // one adapter among these rows, or none
-                const uint32_t at = from + (present ? __ffs(present) - 1 : 0) * kUnit;
-                tmem_ld_32x32(at, *reinterpret_cast<uint32_t(*)[32]>(v));
-                tmem_ld_32x32(at + 32, *reinterpret_cast<uint32_t(*)[32]>(v + 32));
-                tmem_ld_wait();
-            } else {
-                for (int i = 0; i < d; ++i) {
-                    if (!(present >> i & 1)) continue;
+            const uint32_t from = taddr + buf * 256 + (u - step * G) * kUnit;
+            tmem_ld_32x32(from + first * G * kUnit, *reinterpret_cast<uint32_t(*)[32]>(v));
+            tmem_ld_32x32(from + first * G * kUnit + 32, *reinterpret_cast<uint32_t(*)[32]>(v + 32));
+            tmem_ld_wait();
+            for (uint32_t more = present & (present - 1); more; more &= more - 1) {  // another adapter among these rows
+                const int i = __ffs(more) - 1;
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        uint32_t w[16];
-                        tmem_ld_32x16(from + i * kUnit + 16 * h, w);
-                        tmem_ld_wait();
+                for (int h = 0; h < 4; ++h) {
+                    uint32_t w[16];
+                    tmem_ld_32x16(from + i * G * kUnit + 16 * h, w);
+                    tmem_ld_wait();
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) v[16 * h + j] = own == i ? w[j] : v[16 * h + j];
-                    }
+                    for (int j = 0; j < 16; ++j) v[16 * h + j] = own == i ? w[j] : v[16 * h + j];
                 }
             }
             tc_fence_before();
