@@ -296,9 +296,11 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
     BWord bw[kWide ? NR / 4 : 1][4];
     int b_rank = 0;  // of the adapter whose B this is
     Eight next0 = none, next1 = none;
-    auto load_b = [&](int i, int q) {
+    // B of the next tile or the next columns, where there are registers for it
+    constexpr bool kAheadB = NR <= 4;
+    BWord bn[kAheadB ? (kWide ? NR / 4 : 1) : 1][kAheadB ? 4 : 1];
+    auto load_b = [&](auto &to, int i, int q) {
         const int p0 = s.pos[i], r = s.rank[p0];
-        b_rank = r;
         const __half *B = a.B + (size_t)s.slot[p0] * a.stride_b + kLane * t;
 #pragma unroll
         for (int k = 0; k < (kWide ? NR / 4 : 1); ++k) {
@@ -308,7 +310,7 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
                 const int col = q * 32 + (g >> 1) * 8 + 2 * j + (g & 1);
                 BWord w{};
                 if (col < a.N && k0 < (NR <= 2 ? a.max_rank : r)) w = *reinterpret_cast<const BWord *>(B + (size_t)col * a.ldb + 4 * kLane * k);
-                bw[k][j] = w;
+                to[k][j] = w;
             }
         }
     };
@@ -329,7 +331,7 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
         next1 = in && g + 8 < n ? *reinterpret_cast<const Eight *>(base + (size_t)(m0 + s.row[p0 + g + 8]) * a.ldbase + n0) : none;
     };
     if (rounds && tiles) {
-        load_b(0, q0 + warp);
+        load_b(bw, 0, q0 + warp);
         load_base(0, q0 + warp);
     }
     // ---- this CTA's part of T to every CTA of the cluster
@@ -392,16 +394,18 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
     // next of the same adapter, base comes one tile ahead.
     for (int i = 0, q = q0 + warp, fresh = 1, left = rounds * tiles; left > 0; --left) {
         const int p0 = s.pos[i], n = s.count[i];
-        if (!fresh && (i == 0 || s.slot[p0] != s.slot[s.pos[i - 1]])) {
-            load_b(i, q);
-            fresh = 1;
+        if (fresh) {
+            b_rank = s.rank[p0];
+            mask_b();
         }
-        if (fresh) mask_b();
-        fresh = 0;
         [[maybe_unused]] const int r = b_rank;
         const Eight b0 = next0, b1 = next1;
         const int next_i = i + 1 < tiles ? i + 1 : 0, next_q = next_i ? q : q + kWarps;
+        fresh = left > 1 && (next_i == 0 || s.slot[s.pos[next_i]] != s.slot[p0]);
         if (left > 1) load_base(next_i, next_q);
+        if constexpr (kAheadB) {
+            if (fresh) load_b(bn, next_i, next_q);
+        }
         const int n0 = q * 32 + 8 * t;
         float acc[4][4];
 #pragma unroll
@@ -436,6 +440,16 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
         const float o1[8] = {acc[0][2], acc[0][3], acc[1][2], acc[1][3], acc[2][2], acc[2][3], acc[3][2], acc[3][3]};
         if (n0 < a.N && g < n) add_store(Y + (size_t)(m0 + s.row[g0]) * a.ldy + n0, b0, o0, s.factor[g0]);
         if (n0 < a.N && g + 8 < n) add_store(Y + (size_t)(m0 + s.row[g1]) * a.ldy + n0, b1, o1, s.factor[g1]);
+        if (fresh) {
+            if constexpr (kAheadB) {
+#pragma unroll
+                for (int k = 0; k < (kWide ? NR / 4 : 1); ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) bw[k][j] = bn[k][j];
+            } else {
+                load_b(bw, next_i, next_q);
+            }
+        }
         i = next_i;
         q = next_q;
     }
