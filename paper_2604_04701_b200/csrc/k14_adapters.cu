@@ -175,13 +175,13 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
     const int cta = C > 1 ? (int)cluster_ctarank() : 0;
     const int m0 = (int)(blockIdx.x >> log_c) * W, rows = min(W, a.M - m0);
     if constexpr (kBehind) {
-        // k_adapter_tiles lets this kernel start behind its own wait, so what both read is there.  It has done this window, or its
-        // rows are not touched by it; either way this kernel must not end before that one has.
+        // k_adapter_tiles lets this kernel start behind its own wait, so what both read is there.  It has done the 128 rows that these belong to,
+        // or does not touch them; either way this kernel must not end before that one has.
         __shared__ WindowAdapters s_win;
         int mine;
         bool bad;
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-        if (window_adapters(&s_win, a.row_slot, a.rank, a.slots, a.max_rank, m0, a.M, &mine, &bad)) {
+        if (window_adapters(&s_win, a.row_slot, a.rank, a.slots, a.max_rank, m0 / kWindow * kWindow, a.M, &mine, &bad)) {
             asm volatile("griddepcontrol.wait;" ::: "memory");
             return;
         }
@@ -483,11 +483,17 @@ cudaError_t launch_form(const AdapterArgs &a, int sms, cudaStream_t s) {
         }
     }
     // As many CTAs as the device holds two of on an SM: clusters of 8 as long as windows of up to 32 rows make few enough of them, then smaller
-    // ones.  (1 x 768 -> 768 ... FIGURES)
+    // ones.  Behind k_adapter_tiles windows of 128 rows, of 64 or 32 where those would leave SMs idle.
     const auto windows = [&](int rows) { return ((long long)a.M + rows - 1) / rows; };
-    int W = kBehind ? kWindow : 1, log_c = 3;
+    const auto largest = [&](int rows) {  // cluster
+        int l = 3;
+        while (l && (windows(rows) << l > 2 * sms || smem_bytes<NR>(rows, 1 << l) > kSmemMost)) --l;
+        return l;
+    };
+    int W = kBehind ? kWindow : 1;
     while (!kBehind && W < kMostRows && windows(W) * 8 > 2 * sms) W *= 2;
-    while (log_c && (windows(W) << log_c > 2 * sms || smem_bytes<NR>(W, 1 << log_c) > kSmemMost)) --log_c;
+    while (kBehind && W > kMostRows && windows(W) << largest(W) < sms) W /= 2;
+    const int log_c = largest(W);
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(windows(W) << log_c));
     cfg.blockDim = dim3(kT);
