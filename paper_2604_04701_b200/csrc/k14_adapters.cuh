@@ -36,12 +36,12 @@ __device__ __forceinline__ void split(float x, __half *hi, __half *lo) {
 constexpr int kWindow = 128, kWindowAdapters = 4;
 struct WindowAdapters {  // of 128 rows
     int count;           // adapters
+    int uneven;          // whether one of their ranks ends inside a step of 16 that is not the last of max_rank
     int slot[kWindowAdapters], rank[kWindowAdapters];
     int next[kWindowAdapters + 1];
     int8_t index[kWindow];  // by row: which of them, -1 none
 };
-// Whether k_adapter_tiles takes the window that begins at row m0: up to four adapters whose ranks together fit 128 columns of tensor memory, each of
-// them ending at a step of 16 or where all end (beyond max_rank a copy brings zeros; beyond a lower rank anything may stand).  Called by
+// Whether k_adapter_tiles takes the window that begins at row m0: up to four adapters that together fit 128 columns of tensor memory.  Called by
 // all threads of a CTA, at least 128; *mine: the calling thread's row's adapter among the window's.
 __device__ __forceinline__ bool window_adapters(WindowAdapters *w, const int32_t *row_slot, const int32_t *ranks, int slots, int max_rank, int m0, int M,
                                                 int *mine, bool *bad) {
@@ -53,7 +53,7 @@ __device__ __forceinline__ bool window_adapters(WindowAdapters *w, const int32_t
     *bad = false;
     if (tid < kWindow && tid < M - m0) key = adapter_of(row_slot[m0 + tid], ranks, slots, max_rank, &rank, bad);
     const bool uneven = key != INT_MAX && rank % 16 != 0 && rank != max_rank;
-    if (__syncthreads_or(uneven)) return false;
+    const int any_uneven = __syncthreads_or(uneven);
     for (; n <= most; ++n) {
         const int low = __reduce_min_sync(0xffffffffu, key > prev ? key : INT_MAX);
         if ((tid & 31) == 0 && low != INT_MAX) atomicMin(&w->next[n], low);
@@ -68,7 +68,10 @@ __device__ __forceinline__ bool window_adapters(WindowAdapters *w, const int32_t
         }
         prev = cur;
     }
-    if (tid == 0) w->count = n;
+    if (tid == 0) {
+        w->count = n;
+        w->uneven = any_uneven;
+    }
     if (tid < kWindow) w->index[tid] = (int8_t)*mine;
     __syncthreads();
     return true;

@@ -7,7 +7,7 @@
 // tiles, the results are written over it there and leave by TMA, so that no thread addresses global memory and the kernel
 // moves X, base and Y once.  Rows are not sorted: prompts bring an adapter's rows together.
 //
-// Windows that do not suit (too many adapters, a rank that ends inside a step of 16) are left to k_adapters, which runs
+// Windows that do not suit (too many adapters) are left to k_adapters, which runs
 // behind this kernel over all windows and makes the same choice.
 //
 // Roles: warp 0 TMA for X, A, then base; warp 1 products; groups of four warps for the results (one per quarter of the tensor memory's
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
                 const __grid_constant__ CUtensorMap tm_base, const __grid_constant__ CUtensorMap tm_y, const TileParams p) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t x_full[kMaxX], x_empty[kMaxX], b_full[kMaxB], b_empty[kMaxB], base_full[kMaxBase], base_empty[kMaxBase];
+    __shared__ uint64_t x_full[kMaxX], x_empty[kMaxX], b_full[kMaxB], b_even[kMaxB], b_empty[kMaxB], base_full[kMaxBase], base_empty[kMaxBase];
     __shared__ uint64_t t_full, t_ready, acc_full[2], acc_empty[2], drained;
     __shared__ float s_factor[128];
     __shared__ WindowAdapters s_win;
@@ -155,7 +155,7 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kMaxX; ++i) { mbar_init(&x_full[i], 1); mbar_init(&x_empty[i], 1); }
-        for (int i = 0; i < kMaxB; ++i) { mbar_init(&b_full[i], 1); mbar_init(&b_empty[i], 1); }
+        for (int i = 0; i < kMaxB; ++i) { mbar_init(&b_full[i], 1); mbar_init(&b_even[i], 1); mbar_init(&b_empty[i], 1); }
         for (int i = 0; i < kMaxBase; ++i) { mbar_init(&base_full[i], 1); mbar_init(&base_empty[i], 4); }
         mbar_init(&t_full, 1);
         mbar_init(&t_ready, 4);
@@ -220,6 +220,22 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
         // ------------------------------------------------------------ B
         int issued = 0;
         bool ok = true;
+        // What stands beyond a rank that ends inside a step of 16 is set to zero once it has landed: T has zeros there, but it may be no numbers.
+        auto even = [&](int j) {
+            const int s = j % b_stages, rows = min(G, u1 - u0 - j * G) * kUnit;
+            if (!mbar_wait_warp(&b_full[s], (j / b_stages) & 1, abort_flag, p.spin)) return false;
+            for (int i = 0; i < d; ++i) {
+                const int r = s_win.rank[i], end = (r + 15) & ~15;
+                uint8_t *block = sm_b + s * b_stage + (i * R64 + (r >> 6)) * G * (kBox / 2);
+                for (int n = lane; n < rows; n += 32)
+                    for (int k = r; k < end; ++k)
+                        *reinterpret_cast<__half *>(block + n * 128 + (((k & 63) >> 3) ^ (n & 7)) * 16 + (k & 7) * 2) = __float2half_rn(0.0f);
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&b_even[s]);
+            return true;
+        };
         for (; issued * G < u1 - u0 && ok; ++issued) {
             const int s = issued % b_stages, n = min(G, u1 - u0 - issued * G);
             if (!mbar_wait_warp(&b_empty[s], ((issued / b_stages) & 1) ^ 1, abort_flag, p.spin)) { ok = false; break; }
@@ -227,7 +243,9 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
             for (int i = 0; i < d * R64; ++i)
                 for (int k = 0; k < n; ++k)
                     tma_load_3d_elect(sm_b + s * b_stage + (i * G + k) * (kBox / 2), &tm_b, &b_full[s], i % R64 * 64, (u0 + issued * G + k) * kUnit, s_win.slot[i / R64]);
+            if (s_win.uneven && issued) ok = even(issued - 1);
         }
+        if (ok && s_win.uneven) ok = even(issued - 1);
         if (!ok)
             for (int k = issued > b_stages ? issued - b_stages : 0; k < issued; ++k)
                 for (uint32_t i = 0; i < kSpinLimit; ++i)
@@ -262,13 +280,14 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
             mma_commit_elect(&t_full);
             if (!mbar_wait_warp(&t_ready, 0, abort_flag, p.spin)) return false;
             tc_fence_after();
+            const bool uneven = s_win.uneven != 0;
             uint32_t packed = 0;  // steps of 16 ranks of every adapter
 #pragma unroll
             for (int i = 0; i < D; ++i) packed |= (uint32_t)((s_win.rank[i] + 15) >> 4) << (8 * i);
             const uint64_t t_desc = smem_desc_sw128(sm0), b_desc = smem_desc_sw128(sm0 + blocks * 2 * kBox);
             const int count = (u1 - u0 + units_g - 1) / units_g;
             for (int u = 0, st = 0, ph = 0, buf = 0, bph = 1; u < count; ++u) {
-                if (!mbar_wait_warp(&acc_empty[buf], bph, abort_flag, p.spin) || !mbar_wait_warp(&b_full[st], ph, abort_flag, p.spin)) return false;
+                if (!mbar_wait_warp(&acc_empty[buf], bph, abort_flag, p.spin) || !mbar_wait_warp(uneven ? &b_even[st] : &b_full[st], ph, abort_flag, p.spin)) return false;
                 tc_fence_after();
                 auto products = [&](auto blocks_c) {
                     constexpr int kB = decltype(blocks_c)::value, kG = group_units(D, kB == 2);  // blocks of 64 ranks
