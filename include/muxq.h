@@ -361,8 +361,8 @@ int muxq_residual_norm(const void *R, int ldr, int res_kind, const void *Y, int 
  *         on are not used, whatever they hold; rank 0 is a slot without an adapter
  *   scale device fp32 [slots], or NULL: 1
  *   row_slot  device int32 [M]
- *   dev_status  device int32 (sticky): raised to MUXQ_ERR_INVALID_ARG when a used row_slot or rank is out of range; the rows
- *         concerned are then taken as rows without an adapter
+ *   dev_status  device int32 (sticky): raised to MUXQ_ERR_INVALID_ARG when a used row_slot or rank is out of range (the rows
+ *         concerned are then taken as rows without an adapter), to MUXQ_ERR_TIMEOUT when a bounded wait expires (Y then unspecified)
  * Everything is read in stream order (an adapter may be loaded into a slot by work ahead of the call).  Y overlaps nothing but base;
  * rows behind M and columns behind N are left as they are.  Results do not depend on the other rows of the batch but for the order
  * of the sums over K, and are the same from call to call.  K, N, max_rank, pitches and strides are multiples of 8 (pitch of

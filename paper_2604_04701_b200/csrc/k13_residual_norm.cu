@@ -6,6 +6,12 @@
 // written once.  The mean is taken first and the squares of the differences from it second, both from the registers: no
 // cancellation of large sums.  All of it is fp32; H and X are rounded once each (x from h as it is before its own rounding: the
 // fp16 form of the stream costs no accuracy of x).
+//
+// Bound: HBM on long inputs (16384 x 1280, fp32 stream, fp16 Y and gate by rows: 48 us for 294 MB, 6.1 TB/s; 32768 x 768 in fp16 35 us, 5.7),
+// where what counts is that an SM has enough rows under way and that few instructions are spent on each (packed arithmetic on pairs, no
+// divisions, channels addressed from one counter: 87 -> 48 us); by the launch at decode steps (1.7 us in a row of calls).  Tried: CTAs that
+// stay and copy rows ahead into shared memory asynchronously (80 to 140 us: too few warps for the arithmetic); a named barrier for each row
+// of several warps (a kernel that names barriers by number is given all 16 of a CTA, so four CTAs fill an SM).
 #include "../../include/muxq.h"
 #include "kernels.h"
 

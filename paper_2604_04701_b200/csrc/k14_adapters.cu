@@ -8,9 +8,14 @@
 // fp16 numbers whose sum has 22 bits of it: one fp16 number alone would put an error of 2^-11 on an fp32 result, and rows
 // of large activations would leave its range.
 //
-// The matrix instructions are the ones that read registers (m16n8k16): at ranks up to 64 the operator is bound by X, base and Y in HBM,
-// and operands whose order of k may be chosen freely go from global memory to registers in whole 16-byte words without a
-// detour; n is permuted so that a thread ends up with eight neighbouring results.
+// The matrix instructions are the ones that read registers (m16n8k16): the operator is bound by latencies and by memory here, and operands
+// whose order of k may be chosen freely go from global memory to registers in whole 16-byte words without a detour; n is permuted so that a
+// thread ends up with eight neighbouring results.  Long inputs go to k_adapter_tiles first (k15_adapter_tiles.cu).
+//
+// Bound: one chain of latencies at decode steps -- row_slot, then X and A, the parts of T through the cluster, T B^T -- of about 6200 cycles
+// behind the wait for the launch before (1 x 768 -> 768 rank 8 in a row of calls 3.9 us, 16 x 1280 -> 3840 with 16 adapters 5.4); what shaped it, us of the first:
+// 64-bit divisions for a CTA's share of K and N 4.8 -> 4.1, parts of T pushed by stores instead of fetched behind the barrier and rows
+// ordered by one warp 5.9 -> 4.8.  Between, memory: 1003 x 1280 -> 5120 rank 32 20.9 us, its columns of N at 4.8 TB/s.
 #include "../../include/muxq.h"
 #include "k14_adapters.cuh"
 
@@ -157,7 +162,7 @@ __device__ __forceinline__ void order_rows(Tiles<kWindow> *s, int key, int rows)
 }
 
 // kBehind: windows of 128 rows that k_adapter_tiles has left (k15_adapter_tiles.cu).  Larger windows have more rows of an adapter to share its
-// A and B: 12000 rows of 16 adapters in any order, 1280 -> 2560, rank 64: FIGURE.
+// A and B: 12000 rows of 16 adapters in any order, 1280 -> 2560, rank 64: 560 us with windows of 32 rows, 321 with these.
 template <int NR, typename TO, bool kBehind>
 __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterArgs a, int W, int log_c) {
     extern __shared__ __align__(16) uint8_t smem[];

@@ -1,17 +1,26 @@
-// Low-rank adapters (k14_adapters.cu) on long inputs: windows of 128 rows that hold few adapters, on the tensor cores' own memory.
+// Low-rank adapters (k14_adapters.cu) on long inputs: windows of 128 rows that hold few adapters, on tensor memory.
 //
 // A CTA takes 128 consecutive rows and a range of columns.  X and A come by TMA and T = X A^T is accumulated in tensor memory, for every
 // adapter of the window over all its rows (a row's own T is picked from its adapter's columns).  T is scaled and split into two fp16 halves
-// as in k14_adapters.cu and laid down as the left operand of the second product, which runs over 64 columns of N at a time, again once
-// for every adapter into an accumulator of its own: what an adapter holds reaches no row of another.  base comes by TMA into a ring of
-// tiles, the results are written over it there and leave by TMA, so that no thread addresses global memory and the kernel
-// moves X, base and Y once.  Rows are not sorted: prompts bring an adapter's rows together.
+// as in k14_adapters.cu and laid down as the left operand of the second product, which runs over N in steps of 64 columns, once for every
+// adapter into an accumulator of its own: what an adapter holds reaches no row of another.  base comes by TMA into a ring of tiles, the
+// results are written over it there and leave by TMA, so that no thread addresses global memory and the kernel moves X, base and Y
+// once.  Rows are not sorted: prompts bring an adapter's rows together.
 //
-// Windows that do not suit (too many adapters) are left to k_adapters, which runs
-// behind this kernel over all windows and makes the same choice.
+// Windows with more adapters than tensor memory has columns for are left to k_adapters, which runs behind this kernel over all windows and
+// makes the same choice.  Windows without any adapter are copied.
 //
 // Roles: warp 0 TMA for X, A, then base; warp 1 products; groups of four warps for the results (one per quarter of the tensor memory's
-// lanes, the first group also for T), steps of N dealt out in turn so that their chains of latencies overlap; the last warp TMA for B.  Every wait is bounded; on expiry the CTA raises MUXQ_ERR_TIMEOUT, lets its copies and products end and returns.
+// lanes, the first group also for T), steps of N dealt out in turn so that their chains of latencies overlap; the last warp TMA for B.
+// Every wait is bounded; on expiry the CTA raises MUXQ_ERR_TIMEOUT, lets its copies and products end and returns.
+//
+// Bound: HBM from some 8192 rows on (16384 x 1280 -> 5120 at rank 64: 69 us for 378 MB, 5.5 TB/s; the steps of N run at the rate of HBM, but
+// nothing of them overlaps the first product and T, which took 31 of 125 thousand cycles), below that the chain window - T - products
+// with few windows for the device.  Taken from 1024 rows on, k_adapters below, us, here / k_adapters: 1003 x 1280 -> 5120
+// rank 32 20.8 / 20.9, 900 x 2560 -> 2560 21.7 / 14.1, 700 x 1280 -> 1280 14.1 / 9.5; 8192 x 768 -> 2304 22.6 / 46, 16384 rows 73 / 179.
+// Tried: clusters that divide K among the CTAs of a window and exchange T (the exchange costs 7000 cycles: 2000 rows 18.0 -> 19.6 us,
+// 8192 22.8 -> 26.2), eight stages of X instead of four (no change: a stage takes 600 cycles to be issued), three groups of result
+// warps (no change).
 #include <limits.h>
 
 #include <type_traits>

@@ -419,6 +419,52 @@ def test_long_inputs_that_are_not_finite_stay_alone(gpu, value):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,names", [(1, ["k_adapters"]), (1023, ["k_adapters"]), (1024, ["k_adapter_tiles", "k_adapters"])])
+def test_which_kernels_run(gpu, M, names):
+    from conftest import kernels_launched
+    v, whole = _inputs(M, 264, 200, 5, 16, (16, 7), F16)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    call = lambda: gpu.muxq_adapters(v["X"], v["A"], v["B"], v["ids"], status, v["scale"], v["rank"], v["base"], out=whole[:M, :200])
+    call()
+    torch.cuda.synchronize()
+    ran = [name for name, _ in kernels_launched(call)]
+    assert len(ran) == len(names) and all(n in r for n, r in zip(names, ran)), ran
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [3, 200, 1500])
+def test_two_calls_at_once(gpu, M):
+    """No workspace: calls on two streams do not disturb each other."""
+    mx = gpu
+    u, whole = _inputs(M, 776, 392, 6, 24, (24, 11, 16), F32)
+    v, _ = _inputs(M, 776, 392, 6, 24, (24, 11, 16), F32, seed=3)
+    u["ids"] = v["ids"] = _runs(torch.Generator().manual_seed(1), M, 6, (300, 200, 70))
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    args = lambda w: (w["X"], w["A"], w["B"], w["ids"], status, w["scale"], w["rank"], w["base"])
+    want = [mx.muxq_adapters(*args(w)).clone() for w in (u, v)]
+    torch.cuda.synchronize()
+    side = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.empty_like(want[0]) for _ in range(2)]
+    for _ in range(20):
+        for k, w in enumerate((u, v)):
+            with torch.cuda.stream(side[k]):
+                mx.muxq_adapters(*args(w), out=outs[k])
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1]) and int(status) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("R,ranks", [(64, (5, 33, 64, 17)), (40, (37,)), (128, (100, 65))])
+@pytest.mark.parametrize("lengths", ["long", "short"])
+def test_long_inputs_whose_ranks_end_inside_a_step(gpu, lengths, R, ranks):
+    """What stands beyond such a rank is no number (see _inputs), in one window beside adapters of other ranks."""
+    for N in (72, 520, 1992):
+        v, whole = _inputs(1400, 200, N, 4, R, ranks, F32)
+        v["ids"] = _runs(torch.Generator().manual_seed(N), 1400, 4, LENGTHS[lengths])
+        _run(gpu, v, whole)
+
+
+@pytest.mark.gpu
 def test_long_inputs_time_out(gpu):
     """A wait that runs out (the loads of a part of K are left out by a test hook) ends the kernel with a status; the next call is right."""
     mx = gpu
