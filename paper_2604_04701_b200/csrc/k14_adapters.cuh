@@ -34,6 +34,7 @@ __device__ __forceinline__ void split(float x, __half *hi, __half *lo) {
 }
 
 constexpr int kWindow = 128, kWindowAdapters = 4;
+constexpr int kWindowRanks = 256;  // columns of tensor memory for T, and rows of A in two stages
 struct WindowAdapters {  // of 128 rows
     int count;           // adapters
     int uneven;          // whether one of their ranks ends inside a step of 16 that is not the last of max_rank
@@ -41,12 +42,12 @@ struct WindowAdapters {  // of 128 rows
     int next[kWindowAdapters + 1];
     int8_t index[kWindow];  // by row: which of them, -1 none
 };
-// Whether k_adapter_tiles takes the window that begins at row m0: up to four adapters that together fit 128 columns of tensor memory.  Called by
+// Whether k_adapter_tiles takes the window that begins at row m0: up to four adapters that together fit kWindowRanks.  Called by
 // all threads of a CTA, at least 128; *mine: the calling thread's row's adapter among the window's.
 __device__ __forceinline__ bool window_adapters(WindowAdapters *w, const int32_t *row_slot, const int32_t *ranks, int slots, int max_rank, int m0, int M,
                                                 int *mine, bool *bad) {
     const int tid = threadIdx.x, r16 = (max_rank + 15) & ~15;
-    const int most = kWindow / r16 < kWindowAdapters ? kWindow / r16 : kWindowAdapters;
+    const int most = kWindowRanks / r16 < kWindowAdapters ? kWindowRanks / r16 : kWindowAdapters;
     if (tid <= kWindowAdapters) w->next[tid] = INT_MAX;
     int key = INT_MAX, rank = 0, prev = -1, n = 0;
     *mine = -1;

@@ -39,14 +39,15 @@ constexpr int kGroups = 2;                // of four result warps; a group takes
 constexpr int kThreads = 32 * (3 + 4 * kGroups), kWarpB = 2 + 4 * kGroups;
 constexpr int kUnit = 64;                 // columns of N at a time
 constexpr int kBox = 128 * 128;           // bytes of 128 rows x 128 bytes
-constexpr int kXRing = 6 * kBox, kMaxX = 6;  // stages of X, 128 x 64, and A, up to 128 rows of 64
+constexpr int kXRing = 6 * kBox, kMaxX = 6;  // stages of X, 128 x 64, and A, up to 256 rows of 64
 constexpr int kTB = 96 * 1024;            // T (32 or 64 KB) and the ring of B
 constexpr int kMaxB = 4, kMaxBase = 8;
+static_assert(kXRing >= 2 * (kBox + kWindowRanks * 128), "two stages of X and A");
 constexpr int kSmem = kTB + 2 * kBox + kXRing + 1024;  // + alignment
 
 // Steps of N that one instruction of the second product covers, so that T, which it reads from shared memory every time, is read less often:
 // with one step an instruction the kernel was bound by shared memory (T and B 48 KB of 112 KB a step; 82 us at 16384 x 1280 -> 5120).  As many as
-// two accumulators for every adapter have columns for, and two stages of B room.
+// two accumulators for every adapter have columns for, and two stages of an adapter's B room.
 __host__ __device__ constexpr int group_units(int adapters, bool high) { return high || adapters > 2 ? 1 : adapters == 2 ? 2 : 4; }
 
 struct TileParams {
@@ -153,7 +154,7 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
     const uint32_t base_addr = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *sm = smem_raw + (base_addr - smem_u32(smem_raw));
     const int x_stage = kBox + d * R16 * 128, x_stages = min(kXRing / x_stage, kMaxX);
-    const int t_bytes = R64 * 2 * kBox, G = group_units(d, R64 == 2), b_stage = d * R64 * G * (kBox / 2);
+    const int t_bytes = R64 * 2 * kBox, G = group_units(d, R64 == 2), b_stage = R64 * G * (kBox / 2);
     int b_stages = (kTB - t_bytes) / b_stage;
     if (b_stages > kMaxB) b_stages = kMaxB;
     constexpr int kBaseStage = kF32 ? 2 * kBox : kBox;
@@ -226,32 +227,30 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
                     if (__all_sync(0xffffffffu, mbar_try_wait(&base_full[k % kBaseStages], (k / kBaseStages) & 1))) break;
         }
     } else if (warp == kWarpB) {
-        // ------------------------------------------------------------ B
+        // ------------------------------------------------------------ B, one adapter's for G steps of N at a time
+        const int all = (u1 - u0 + G - 1) / G * d;
         int issued = 0;
         bool ok = true;
         // What stands beyond a rank that ends inside a step of 16 is set to zero once it has landed: T has zeros there, but it may be no numbers.
         auto even = [&](int j) {
-            const int s = j % b_stages, rows = min(G, u1 - u0 - j * G) * kUnit;
+            const int s = j % b_stages, rows = min(G, u1 - u0 - j / d * G) * kUnit, r = s_win.rank[j % d], end = (r + 15) & ~15;
             if (!mbar_wait_warp(&b_full[s], (j / b_stages) & 1, abort_flag, p.spin)) return false;
-            for (int i = 0; i < d; ++i) {
-                const int r = s_win.rank[i], end = (r + 15) & ~15;
-                uint8_t *block = sm_b + s * b_stage + (i * R64 + (r >> 6)) * G * (kBox / 2);
-                for (int n = lane; n < rows; n += 32)
-                    for (int k = r; k < end; ++k)
-                        *reinterpret_cast<__half *>(block + n * 128 + (((k & 63) >> 3) ^ (n & 7)) * 16 + (k & 7) * 2) = __float2half_rn(0.0f);
-            }
+            uint8_t *block = sm_b + s * b_stage + (r >> 6) * G * (kBox / 2);
+            for (int n = lane; n < rows; n += 32)
+                for (int k = r; k < end; ++k)
+                    *reinterpret_cast<__half *>(block + n * 128 + (((k & 63) >> 3) ^ (n & 7)) * 16 + (k & 7) * 2) = __float2half_rn(0.0f);
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(&b_even[s]);
             return true;
         };
-        for (; issued * G < u1 - u0 && ok; ++issued) {
-            const int s = issued % b_stages, n = min(G, u1 - u0 - issued * G);
+        for (; issued < all && ok; ++issued) {
+            const int s = issued % b_stages, u = issued / d * G, n = min(G, u1 - u0 - u);
             if (!mbar_wait_warp(&b_empty[s], ((issued / b_stages) & 1) ^ 1, abort_flag, p.spin)) { ok = false; break; }
-            mbar_expect_tx_elect(&b_full[s], d * R64 * n * (kBox / 2));
-            for (int i = 0; i < d * R64; ++i)
+            mbar_expect_tx_elect(&b_full[s], R64 * n * (kBox / 2));
+            for (int blk = 0; blk < R64; ++blk)
                 for (int k = 0; k < n; ++k)
-                    tma_load_3d_elect(sm_b + s * b_stage + (i * G + k) * (kBox / 2), &tm_b, &b_full[s], i % R64 * 64, (u0 + issued * G + k) * kUnit, s_win.slot[i / R64]);
+                    tma_load_3d_elect(sm_b + s * b_stage + (blk * G + k) * (kBox / 2), &tm_b, &b_full[s], blk * 64, (u0 + u + k) * kUnit, s_win.slot[issued % d]);
             if (s_win.uneven && issued) ok = even(issued - 1);
         }
         if (ok && s_win.uneven) ok = even(issued - 1);
@@ -270,7 +269,7 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
             constexpr int D = decltype(number)::value;
             const int r16 = (p.max_rank + 15) & ~15, blocks = p.max_rank > 64 ? 2 : 1;
             const int xb = kBox + D * r16 * 128, xs = min(kXRing / xb, kMaxX);
-            const int units_g = group_units(D, blocks == 2), bb = D * blocks * units_g * (kBox / 2), bs = min((kTB - blocks * 2 * kBox) / bb, kMaxB);
+            const int units_g = group_units(D, blocks == 2), bb = blocks * units_g * (kBox / 2), bs = min((kTB - blocks * 2 * kBox) / bb, kMaxB);
             const uint32_t idesc_t = idesc_f16(r16), idesc_y = idesc_f16(units_g * kUnit);
             const uint64_t x_desc = smem_desc_sw128(sm0 + kTB + 2 * kBox);
             for (int c = 0, st = 0, ph = 0; c < chunks; ++c) {
@@ -296,28 +295,30 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
             const uint64_t t_desc = smem_desc_sw128(sm0), b_desc = smem_desc_sw128(sm0 + blocks * 2 * kBox);
             const int count = (u1 - u0 + units_g - 1) / units_g;
             for (int u = 0, st = 0, ph = 0, buf = 0, bph = 1; u < count; ++u) {
-                if (!mbar_wait_warp(&acc_empty[buf], bph, abort_flag, p.spin) || !mbar_wait_warp(uneven ? &b_even[st] : &b_full[st], ph, abort_flag, p.spin)) return false;
+                if (!mbar_wait_warp(&acc_empty[buf], bph, abort_flag, p.spin)) return false;
                 tc_fence_after();
-                auto products = [&](auto blocks_c) {
+                auto products = [&](auto blocks_c, int i) {
                     constexpr int kB = decltype(blocks_c)::value, kG = group_units(D, kB == 2);  // blocks of 64 ranks
+                    const int steps = packed >> (8 * i) & 0xff;
+                    const uint64_t bd = b_desc + (uint64_t)(uint32_t)(st * (bb >> 4));
 #pragma unroll
-                    for (int i = 0; i < D; ++i) {
-                        const int steps = packed >> (8 * i) & 0xff;
-                        const uint64_t bd = b_desc + (uint64_t)(uint32_t)(st * (bb >> 4) + i * kB * kG * (kBox >> 5));
+                    for (int half = 0; half < 2; ++half)
 #pragma unroll
-                        for (int half = 0; half < 2; ++half)
-#pragma unroll
-                            for (int k = 0; k < 4 * kB; ++k)
-                                if (k < steps)
-                                    mma_f16_elect(buf * 256 + i * kG * kUnit, t_desc + (uint64_t)((half * kB + (k >> 2)) * (kBox >> 4) + (k & 3) * 2),
-                                                  bd + (uint64_t)((k >> 2) * kG * (kBox >> 5) + (k & 3) * 2), idesc_y, half || k ? 1u : 0u);
-                    }
+                        for (int k = 0; k < 4 * kB; ++k)
+                            if (k < steps)
+                                mma_f16_elect(buf * 256 + i * kG * kUnit, t_desc + (uint64_t)((half * kB + (k >> 2)) * (kBox >> 4) + (k & 3) * 2),
+                                              bd + (uint64_t)((k >> 2) * kG * (kBox >> 5) + (k & 3) * 2), idesc_y, half || k ? 1u : 0u);
                 };
-                if (blocks == 1) products(std::integral_constant<int, 1>{});
-                else products(std::integral_constant<int, 2>{});
-                mma_commit_elect(&b_empty[st]);
+#pragma unroll
+                for (int i = 0; i < D; ++i) {
+                    if (!mbar_wait_warp(uneven ? &b_even[st] : &b_full[st], ph, abort_flag, p.spin)) return false;
+                    tc_fence_after();
+                    if (blocks == 1) products(std::integral_constant<int, 1>{}, i);
+                    else products(std::integral_constant<int, 2>{}, i);
+                    mma_commit_elect(&b_empty[st]);
+                    if (++st == bs) { st = 0; ph ^= 1; }
+                }
                 mma_commit_elect(&acc_full[buf]);
-                if (++st == bs) { st = 0; ph ^= 1; }
                 if (++buf == 2) { buf = 0; bph ^= 1; }
             }
             return true;
