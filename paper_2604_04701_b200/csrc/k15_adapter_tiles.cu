@@ -535,10 +535,19 @@ bool launch_adapter_tiles(const AdapterArgs &a, cudaStream_t s, cudaError_t *e) 
     p.dev_status = a.dev_status;
     p.spin = test_hooks().spin_limit ? test_hooks().spin_limit : kSpinLimit;
     p.skip_chunk = test_hooks().gemm_skip_kb - 1;
-    const int tiles = (int)(((long long)a.M + 127) / 128), units = (a.N + kUnit - 1) / kUnit;
-    int parts = sms / tiles;
-    if (parts > units) parts = units;
-    if (parts < 1) parts = 1;
+    // CTAs that share a window's columns: the fewest cycles of the fullest SM, each CTA doing all of the first product (cycles by the kernel's own
+    // clock).  More of them than the device holds at once only where that is clearly less: 10525 rows, 1448 -> 3880 at rank 128 in fp32 107 -> 99 us,
+    // 10000 rows, 1280 -> 3840, 51.6 -> 50.3, but 12000 rows, 768 -> 2560, 38.1 -> 39.4 where the estimate gained 2 %.
+    const int units = (a.N + kUnit - 1) / kUnit, chunks = (a.K + 63) / 64;
+    const long long tiles = ((long long)a.M + 127) / 128;
+    int parts = 1;
+    double best = 0.0;
+    for (int n = 1; n <= units && (n == 1 || tiles * n <= 4 * sms); ++n) {
+        const double cost = (double)((tiles * n + sms - 1) / sms) * (5000.0 + 700.0 * chunks + (f32 ? 2000.0 : 1200.0) * ((units + n - 1) / n));
+        if (n > 1 && cost >= (tiles * n > sms ? 0.95 : 1.0) * best) continue;
+        best = cost;
+        parts = n;
+    }
     *e = f32 ? launch_form<true>(a, m, p, parts, s) : launch_form<false>(a, m, p, parts, s);
     return true;
 }
