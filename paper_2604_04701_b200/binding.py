@@ -267,7 +267,7 @@ def muxq_linear(X: torch.Tensor, w_q: torch.Tensor, s_w: torch.Tensor, p: MuxqPa
                 bias: Optional[torch.Tensor] = None, adapters: Optional["Adapters"] = None) -> torch.Tensor:
     """Y = MUXQ-quantized X.W [+ bias] [+ the adapters of the rows' requests]; w_q [N,K] int8 and s_w from
     muxq_quantize(is_weight=True); bias fp32 [N].  The adapters are a call of muxq_adapters behind the layer, added to Y in place
-    (an fp16 Y is rounded before and behind them)."""
+    (an fp16 Y is rounded before and behind them); Y must then lie apart from X."""
     Y = out if out is not None else _alloc_out(X.shape[0], w_q.shape[0], out_kind, X.device)
     if adapters is not None and out_kind == MUXQ_OUT_ACC_I32:
         raise MuxqError("muxq_adapters", MUXQ_ERR_INVALID_ARG)  # they belong to the dequantized output
