@@ -257,21 +257,27 @@ __global__ void __launch_bounds__(kT, NR > 8 ? 1 : 2) k_adapters(const AdapterAr
                     xv[d] = v[d];
                 }
                 load_x(c + kAhead * slices);
+                constexpr int kA = NR <= 4 ? kAhead : 1;  // chunks whose A is on its way at once
 #pragma unroll
-                for (int d = 0; d < kAhead; ++d) {
-                    const int cc = c + d * slices;
-                    if (cc >= c1) break;
-                    const bool in = cc * 32 + 8 * t < a.K;
-                    uint4 w[NR];
+                for (int d = 0; d < kAhead; d += kA) {
+                    if (kA == 1 && c + d * slices >= c1) break;
+                    uint4 w[kA][NR];
 #pragma unroll
-                    for (int j = 0; j < NR; ++j) w[j] = in && j * 8 < r ? *reinterpret_cast<const uint4 *>(A + (size_t)j * 8 * a.lda + cc * 32) : z;
+                    for (int e = 0; e < kA; ++e) {
+                        const int cc = c + (d + e) * slices;
+                        const bool in = cc < c1 && cc * 32 + 8 * t < a.K;
 #pragma unroll
-                    for (int j = 0; j < NR; ++j) {
-                        if (j * 8 < r) {
-                            mma16816(acc[j], xu[d].x, xv[d].x, xu[d].y, xv[d].y, w[j].x, w[j].y);
-                            mma16816(acc[j], xu[d].z, xv[d].z, xu[d].w, xv[d].w, w[j].z, w[j].w);
-                        }
+                        for (int j = 0; j < NR; ++j) w[e][j] = in && j * 8 < r ? *reinterpret_cast<const uint4 *>(A + (size_t)j * 8 * a.lda + cc * 32) : z;
                     }
+#pragma unroll
+                    for (int e = 0; e < kA; ++e)
+#pragma unroll
+                        for (int j = 0; j < NR; ++j) {
+                            if (j * 8 < r) {
+                                mma16816(acc[j], xu[d + e].x, xv[d + e].x, xu[d + e].y, xv[d + e].y, w[e][j].x, w[e][j].y);
+                                mma16816(acc[j], xu[d + e].z, xv[d + e].z, xu[d + e].w, xv[d + e].w, w[e][j].z, w[e][j].w);
+                            }
+                        }
                 }
             }
             float *to = part + (size_t)(wk * active + p0) * kPP + 2 * t;
