@@ -337,7 +337,7 @@ int muxq_linear_decode_noalloc(const void *X_f16, int M, int K, int ldx, const i
  * H and X overlap nothing else that the call reads or writes (columns of one wider matrix that lie side by side do not overlap).
  * Rows behind M and columns behind D are left as they are.  D % 8 == 0, D <= 16384; pitches are multiples of 8 (fp16) or 4 (fp32)
  * elements, all addresses 16-byte aligned.  No workspace.  Everything is read in stream order.  Values beyond the finite ones make
- * their own row unspecified and no other; h^2 must not leave fp32 (|h| < 1e18).
+ * their own row unspecified and no other, and so do values of 1e18 and more where a norm squares them (h under pre, Y under post).
  */
 typedef enum { MUXQ_NORM_NONE = 0, MUXQ_NORM_RMS = 1, MUXQ_NORM_LAYER = 2 } muxq_norm_kind;
 typedef struct muxq_norm {

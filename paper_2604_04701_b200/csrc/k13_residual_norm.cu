@@ -85,7 +85,11 @@ __device__ __forceinline__ Four normalize(Four (&v)[V], const NormSpec &n, float
     Four q = v[0] * v[0];
 #pragma unroll
     for (int i = 1; i < V; ++i) q = fma4(v[i], v[i], q);
-    return four(rsqrtf(__fmaf_rn(sum((q.a.x + q.a.y) + (q.b.x + q.b.y)), inv_d, n.eps)));  // (off by 2 units at most)
+    // D squares of finite values may add up to more than fp32 holds.  The shares of the threads are therefore added 2^-8 times as large: up to 1e18 the
+    // sum is then at most 16384 x 1e36 / 256, and a share (40 squares, of up to 2e18 where the mean is at one end) fits as it is.  Nothing is rounded
+    // by it but shares below 2^-118, which moves the mean square by less than 2^-144.
+    const float mean = __fmaf_rn(sum(((q.a.x + q.a.y) + (q.b.x + q.b.y)) * 0x1p-8f), inv_d * 0x1p8f, n.eps);
+    return four(rsqrtf(mean));  // (off by 2 units at most)
 }
 
 // v <- v r weight + bias; the vectors come from memory where they have not been fetched ahead

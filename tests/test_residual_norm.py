@@ -386,3 +386,36 @@ def test_offsets_beyond_32_bits(gpu):
     n = mx.Norm(RMS)
     want = mx.muxq_residual_norm(R.contiguous(), None, n)[1]
     assert torch.equal(mx.muxq_residual_norm(R, None, n)[1], want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [RMS, LAYER])
+@pytest.mark.parametrize("M,D", [(5, 64), (5, 768), (700, 768), (700, 1280), (5, 5120), (600, 5120), (3, 16384), (600, 16384)])
+def test_up_to_the_largest_values(gpu, M, D, kind):
+    """Rows of values up to 1e18, whose squares add up to more than fp32 holds (D x 1e36), as the stream and as a block's result under post; the mean
+    is near zero, or all but a few values are at the other end, 2e18 from them.  (What keeps the sum within fp32 is a power of two and rounds nothing.)"""
+    mx = gpu
+    gen = torch.Generator().manual_seed(M + D)
+    v = (torch.rand(M, D, generator=gen) * 1.5 + 0.5) * 0.49e18 * (torch.randint(0, 2, (M, D), generator=gen) * 2.0 - 1.0)
+    v[1] = -0.99e18
+    v[1, :3] = 0.99e18
+    v[2] = 0.99e18 * (torch.arange(D) % 2 * 2.0 - 1.0)
+    v = v.cuda()
+    n = mx.Norm(kind, _vec(gen, D), _vec(gen, D, 0.0), 1e-5)
+    _, _, x, ex = reference(v, None, n, None, None, 1, 1.0)
+    check(mx.muxq_residual_norm(v, None, n)[1], torch.float16, x, ex, "x")
+    h, e, _, _ = reference(None, v, None, n, None, 1, 1.0)
+    check(mx.muxq_residual_norm(None, v, None, post=n, want_x=False)[0], torch.float32, h, e, "h")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [RMS, LAYER])
+@pytest.mark.parametrize("M,D", [(3, 768), (600, 768), (3, 16384)])
+def test_a_small_eps_and_values_beside_it(gpu, M, D, kind):
+    """Squares far below those of activations, and an eps that does not cover them."""
+    mx = gpu
+    gen = torch.Generator().manual_seed(D + M)
+    v = (torch.randn(M, D, generator=gen) * 1e-15).cuda()
+    n = mx.Norm(kind, _vec(gen, D), None, 1e-32)
+    _, _, x, ex = reference(v, None, n, None, None, 1, 1.0)
+    check(mx.muxq_residual_norm(v, None, n)[1], torch.float16, x, ex, "x")
