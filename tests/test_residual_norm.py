@@ -419,3 +419,20 @@ def test_a_small_eps_and_values_beside_it(gpu, M, D, kind):
     n = mx.Norm(kind, _vec(gen, D), None, 1e-32)
     _, _, x, ex = reference(v, None, n, None, None, 1, 1.0)
     check(mx.muxq_residual_norm(v, None, n)[1], torch.float16, x, ex, "x")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,D", [(4, 264), (700, 776), (700, 1040), (40, 2560), (650, 5120), (600, 8192)])
+@pytest.mark.parametrize("kind", [RMS, LAYER])
+@pytest.mark.parametrize("weight,bias", [(True, True), (True, False), (False, True), (False, False)])
+def test_weight_and_bias_each_alone(gpu, M, D, kind, weight, bias):
+    """On both sides of the block and for either norm, with few and many channels a thread."""
+    mx = gpu
+    gen = torch.Generator().manual_seed(3 * M + D)
+    R, Y = torch.randn(M, D, generator=gen).cuda(), torch.randn(M, D, generator=gen).half().cuda()
+    norm = lambda: mx.Norm(kind, _vec(gen, D) if weight else None, _vec(gen, D, 0.3) if bias else None, 1e-5)
+    pre, post = norm(), norm()
+    H, X = mx.muxq_residual_norm(R, Y, pre, post=post, scale=0.7)
+    h, e, x, ex = reference(R, Y, pre, post, None, 1, 0.7)
+    check(H, F32, h, e, "h")
+    check(X, F16, x, ex, "x")
