@@ -378,6 +378,10 @@ typedef struct muxq_adapter_set {
 } muxq_adapter_set;
 int muxq_adapters(const void *X_f16, int M, int K, int ldx, const muxq_adapter_set *set, const int32_t *row_slot, int N,
                   const void *base, int ldbase, void *Y, int ldy, int out_kind, int32_t *dev_status, void *stream);
+/* Whether muxq_adapters would take these arguments (MUXQ_OK or its code); nothing is read or launched.  For a caller that launches what
+ * makes base first and wants neither or both. */
+int muxq_adapters_check(const void *X_f16, int M, int K, int ldx, const muxq_adapter_set *set, const int32_t *row_slot, int N,
+                        const void *base, int ldbase, const void *Y, int ldy, int out_kind, const int32_t *dev_status);
 
 /* Synchronizes `stream` and returns the device status word (or MUXQ_ERR_CUDA). */
 int muxq_read_status(const int32_t *dev_status, void *stream);

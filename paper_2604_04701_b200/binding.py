@@ -25,7 +25,7 @@ EXPORTS = (
     "muxq_host_workspace_bytes", "muxq_workspace_init", "muxq_workspace_view", "muxq_detect_outliers", "muxq_build_aux",
     "muxq_quantize", "muxq_gemm", "muxq_linear", "muxq_linear_bias", "muxq_linear_events", "muxq_linear_host",
     "muxq_linear_decode_noalloc", "muxq_int8_mma_peak", "muxq_test_hooks", "muxq_test_late_warps", "muxq_read_status",
-    "muxq_residual_norm", "muxq_adapters", "muxq_chain_plan_bytes", "muxq_chain_device_bytes", "muxq_chain_build", "muxq_chain_run",
+    "muxq_residual_norm", "muxq_adapters", "muxq_adapters_check", "muxq_chain_plan_bytes", "muxq_chain_device_bytes", "muxq_chain_build", "muxq_chain_run",
     "muxq_status_string",
 )
 
@@ -104,6 +104,7 @@ def lib() -> ctypes.CDLL:
         L.muxq_test_late_warps.argtypes = [ctypes.c_uint32]; L.muxq_test_late_warps.restype = i
         L.muxq_residual_norm.argtypes = [vp, i, i, vp, i, i, vp, vp, i, i, i, f, vp, i, i, vp, i, vp, i, vp]; L.muxq_residual_norm.restype = i
         L.muxq_adapters.argtypes = [vp, i, i, i, vp, vp, i, vp, i, vp, i, i, vp, vp]; L.muxq_adapters.restype = i
+        L.muxq_adapters_check.argtypes = [vp, i, i, i, vp, vp, i, vp, i, vp, i, i, vp]; L.muxq_adapters_check.restype = i
         L.muxq_chain_plan_bytes.argtypes = [i]; L.muxq_chain_plan_bytes.restype = sz
         L.muxq_chain_device_bytes.argtypes = [vp, i, i]; L.muxq_chain_device_bytes.restype = sz
         L.muxq_chain_build.argtypes = [vp, i, i, pp, i, vp, sz, vp, sz, vp]; L.muxq_chain_build.restype = i
@@ -114,7 +115,7 @@ def lib() -> ctypes.CDLL:
         at = lambda entry: ctypes.cast(entry, vp).value
         calls.bind(at(L.muxq_linear), at(L.muxq_linear_bias), at(L.muxq_quantize), torch._C._cuda_getDevice,
                    torch._C._cuda_getCurrentRawStream, torch.float16, torch.float32, at(L.muxq_residual_norm),
-                   at(L.muxq_adapters), torch.int32)
+                   at(L.muxq_adapters), torch.int32, at(L.muxq_adapters_check))
         _calls = calls  # first: a thread that finds _lib set goes on to use it
         _lib = L
     return _lib
@@ -267,10 +268,17 @@ def muxq_linear(X: torch.Tensor, w_q: torch.Tensor, s_w: torch.Tensor, p: MuxqPa
                 bias: Optional[torch.Tensor] = None, adapters: Optional["Adapters"] = None) -> torch.Tensor:
     """Y = MUXQ-quantized X.W [+ bias] [+ the adapters of the rows' requests]; w_q [N,K] int8 and s_w from
     muxq_quantize(is_weight=True); bias fp32 [N].  The adapters are a call of muxq_adapters behind the layer, added to Y in place
-    (an fp16 Y is rounded before and behind them); Y must then lie apart from X."""
+    (an fp16 Y is rounded before and behind them); Y must then lie apart from X.  Adapters that do not fit are refused before the
+    layer runs."""
     Y = out if out is not None else _alloc_out(X.shape[0], w_q.shape[0], out_kind, X.device)
-    if adapters is not None and out_kind == MUXQ_OUT_ACC_I32:
-        raise MuxqError("muxq_adapters", MUXQ_ERR_INVALID_ARG)  # they belong to the dequantized output
+    if adapters is not None:
+        if out_kind == MUXQ_OUT_ACC_I32:
+            raise MuxqError("muxq_adapters", MUXQ_ERR_INVALID_ARG)  # they belong to the dequantized output
+        if Y.dtype != (torch.float32 if out_kind == MUXQ_OUT_F32 else torch.float16):
+            raise ValueError("out: the type of out_kind is wanted")
+        rc = _hot().adapters_check(X, adapters.A, adapters.B, adapters.row_slot, adapters.scale, adapters.rank, Y, Y, ws.status)
+        if rc:
+            raise MuxqError("muxq_adapters", rc)
     rc = _hot().linear(X, w_q, s_w, p, ws.buf, ws.status, out_kind, Y, bias)
     if rc:
         raise MuxqError("muxq_linear" if bias is None else "muxq_linear_bias", rc)

@@ -597,8 +597,8 @@ int muxq_residual_norm(const void *R, int ldr, int res_kind, const void *Y, int 
     return cuda_rc(launch_residual_norm(a, static_cast<cudaStream_t>(stream)));
 }
 
-int muxq_adapters(const void *X, int M, int K, int ldx, const muxq_adapter_set *set, const int32_t *row_slot, int N,
-                  const void *base, int ldbase, void *Y, int ldy, int out_kind, int32_t *dev_status, void *stream) {
+int muxq_adapters_check(const void *X, int M, int K, int ldx, const muxq_adapter_set *set, const int32_t *row_slot, int N,
+                        const void *base, int ldbase, const void *Y, int ldy, int out_kind, const int32_t *dev_status) {
     if (!X || !set || !set->A_f16 || !set->B_f16 || !row_slot || !Y || !dev_status || M <= 0 || K <= 0 || N <= 0 || set->slots <= 0 ||
         set->max_rank <= 0 || ldx < K || set->lda < K || set->ldb < set->max_rank || ldy < N || (base && ldbase < N) || !real_kind(out_kind) ||
         (set->slots > 1 && (set->stride_a < (int64_t)(set->max_rank - 1) * set->lda + K || set->stride_b < (int64_t)(N - 1) * set->ldb + set->max_rank)))
@@ -615,6 +615,13 @@ int muxq_adapters(const void *X, int M, int K, int ldx, const muxq_adapter_set *
     if ((overlap(y, b) && !same_place(y, b)) || overlap(y, x) || overlap(y, wa) || overlap(y, wb) || overlap(y, ids) || overlap(y, sc) ||
         overlap(y, rk))
         return MUXQ_ERR_INVALID_ARG;
+    return MUXQ_OK;
+}
+
+int muxq_adapters(const void *X, int M, int K, int ldx, const muxq_adapter_set *set, const int32_t *row_slot, int N,
+                  const void *base, int ldbase, void *Y, int ldy, int out_kind, int32_t *dev_status, void *stream) {
+    const int rc = muxq_adapters_check(X, M, K, ldx, set, row_slot, N, base, ldbase, Y, ldy, out_kind, dev_status);
+    if (rc != MUXQ_OK) return rc;
     AdapterArgs a{};
     a.X = static_cast<const __half *>(X);
     a.M = M; a.K = K; a.ldx = ldx;

@@ -24,12 +24,15 @@ typedef int (*residual_norm_fn)(const void *, int, int, const void *, int, int, 
 
 typedef int (*adapters_fn)(const void *, int, int, int, const muxq_adapter_set *, const int32_t *, int, const void *, int, void *, int, int,
                            int32_t *, void *);
+typedef int (*adapters_check_fn)(const void *, int, int, int, const muxq_adapter_set *, const int32_t *, int, const void *, int, const void *, int,
+                                 int, const int32_t *);
 
 static linear_fn f_linear;
 static linear_bias_fn f_linear_bias;
 static quantize_fn f_quantize;
 static residual_norm_fn f_residual_norm;
 static adapters_fn f_adapters;
+static adapters_check_fn f_adapters_check;
 static PyObject *get_device, *raw_stream, *dt_f16, *dt_f32, *dt_i32;
 static PyObject *n_data_ptr, *n_shape, *n_stride, *n_dtype, *n_is_cuda, *n_numel, *n_is_contiguous, *n_get_device;
 static PyObject *n_threshold, *n_exp_factor, *n_act_bits, *n_w_bits, *n_gran, *n_aux_scale, *n_max_outliers;
@@ -338,42 +341,58 @@ static int vector_i32(PyObject *t, const char *what, int device, int len, const 
     return 0;
 }
 
-/* adapters(X, A, B, row_slot, scale or None, rank or None, base or None, Y, status) -> status code */
-static PyObject *adapters(PyObject *self, PyObject *const *a, Py_ssize_t n) {
-    if (n != 9) return PyErr_Format(PyExc_TypeError, "adapters takes 9 arguments");
-    operand x = {0}, b = {0}, y = {0};
-    muxq_adapter_set set = {0};
-    void *s;
+typedef struct {
+    operand x, base, y;
+    muxq_adapter_set set;
     const int32_t *row_slot, *status;
-    int device, K, N, slots, rank;
-    if (current_place(&device, &s) || operand_of(a[0], "X", device, 1 << 2, &x) ||
-        stack_of(a[1], "A", device, &set.A_f16, &set.slots, &set.max_rank, &K, &set.lda, &set.stride_a) ||
-        stack_of(a[2], "B", device, &set.B_f16, &slots, &N, &rank, &set.ldb, &set.stride_b))
-        return NULL;
-    if (x.kind != MUXQ_OUT_F16) return refuse("X", "fp16 is wanted"), NULL;
-    if (x.cols != K) return refuse("A", "the shape does not fit X"), NULL;
-    if (slots != set.slots || rank != set.max_rank) return refuse("B", "the shape does not fit A"), NULL;
-    if (matrix_of(a[7], "Y", device, x.rows, N, &y) || (a[6] != Py_None && matrix_of(a[6], "base", device, x.rows, N, &b)) ||
-        vector_i32(a[3], "row_slot", device, x.rows, &row_slot) || vector_f32(a[4], "scale", device, slots, &set.scale) ||
-        vector_i32(a[5], "rank", device, slots, &set.rank) || vector_i32(a[8], "status", device, -1, &status))
-        return NULL;
-    if (a[6] != Py_None && b.kind != y.kind) return refuse("base", "the type of Y is wanted"), NULL;
+    int K, N;
+    void *stream;
+} adapter_operands;
+/* X, A, B, row_slot, scale or None, rank or None, base or None, Y, status */
+static int adapter_operands_of(PyObject *const *a, Py_ssize_t n, adapter_operands *o) {
+    int device, slots, rank;
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "the adapters' calls take 9 arguments"), -1;
+    memset(o, 0, sizeof *o);
+    if (current_place(&device, &o->stream) || operand_of(a[0], "X", device, 1 << 2, &o->x) ||
+        stack_of(a[1], "A", device, &o->set.A_f16, &o->set.slots, &o->set.max_rank, &o->K, &o->set.lda, &o->set.stride_a) ||
+        stack_of(a[2], "B", device, &o->set.B_f16, &slots, &o->N, &rank, &o->set.ldb, &o->set.stride_b))
+        return -1;
+    if (o->x.kind != MUXQ_OUT_F16) return refuse("X", "fp16 is wanted");
+    if (o->x.cols != o->K) return refuse("A", "the shape does not fit X");
+    if (slots != o->set.slots || rank != o->set.max_rank) return refuse("B", "the shape does not fit A");
+    if (matrix_of(a[7], "Y", device, o->x.rows, o->N, &o->y) || (a[6] != Py_None && matrix_of(a[6], "base", device, o->x.rows, o->N, &o->base)) ||
+        vector_i32(a[3], "row_slot", device, o->x.rows, &o->row_slot) || vector_f32(a[4], "scale", device, slots, &o->set.scale) ||
+        vector_i32(a[5], "rank", device, slots, &o->set.rank) || vector_i32(a[8], "status", device, -1, &o->status))
+        return -1;
+    return a[6] != Py_None && o->base.kind != o->y.kind ? refuse("base", "the type of Y is wanted") : 0;
+}
+/* adapters(the operands) -> status code */
+static PyObject *adapters(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    adapter_operands o;
+    if (adapter_operands_of(a, n, &o)) return NULL;
     int rc;
     Py_BEGIN_ALLOW_THREADS
-    rc = f_adapters(x.ptr, x.rows, K, x.ld, &set, row_slot, N, b.ptr, b.ld, y.ptr, y.ld, y.kind, (int32_t *)status, s);
+    rc = f_adapters(o.x.ptr, o.x.rows, o.K, o.x.ld, &o.set, o.row_slot, o.N, o.base.ptr, o.base.ld, o.y.ptr, o.y.ld, o.y.kind, (int32_t *)o.status, o.stream);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
 }
+/* adapters_check(the operands) -> the status code that adapters would give for them; nothing is launched */
+static PyObject *adapters_check(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    adapter_operands o;
+    if (adapter_operands_of(a, n, &o)) return NULL;
+    return PyLong_FromLong(f_adapters_check(o.x.ptr, o.x.rows, o.K, o.x.ld, &o.set, o.row_slot, o.N, o.base.ptr, o.base.ld, o.y.ptr, o.y.ld, o.y.kind, o.status));
+}
 
 /* bind(muxq_linear, muxq_linear_bias, muxq_quantize, get_device, raw_stream, float16, float32[, muxq_residual_norm[,
- * muxq_adapters, int32]]) */
+ * muxq_adapters, int32[, muxq_adapters_check]]]) */
 static PyObject *bind(PyObject *self, PyObject *const *a, Py_ssize_t n) {
-    if (n != 7 && n != 8 && n != 10) return PyErr_Format(PyExc_TypeError, "bind takes 7, 8 or 10 arguments");
+    if (n != 7 && n != 8 && n != 10 && n != 11) return PyErr_Format(PyExc_TypeError, "bind takes 7, 8, 10 or 11 arguments");
     f_linear = (linear_fn)PyLong_AsVoidPtr(a[0]);
     f_linear_bias = (linear_bias_fn)PyLong_AsVoidPtr(a[1]);
     f_quantize = (quantize_fn)PyLong_AsVoidPtr(a[2]);
     if (n > 7) f_residual_norm = (residual_norm_fn)PyLong_AsVoidPtr(a[7]);
     if (n > 8) f_adapters = (adapters_fn)PyLong_AsVoidPtr(a[8]);
+    if (n > 10) f_adapters_check = (adapters_check_fn)PyLong_AsVoidPtr(a[10]);
     if (PyErr_Occurred()) return NULL;
     Py_XSETREF(get_device, Py_NewRef(a[3]));
     Py_XSETREF(raw_stream, Py_NewRef(a[4]));
@@ -388,6 +407,7 @@ static PyMethodDef methods[] = {
     {"linear", (PyCFunction)(void (*)(void))linear, METH_FASTCALL, "muxq_linear / muxq_linear_bias"},
     {"quantize_weight", (PyCFunction)(void (*)(void))quantize_weight, METH_FASTCALL, "muxq_quantize(is_weight = 1)"},
     {"adapters", (PyCFunction)(void (*)(void))adapters, METH_FASTCALL, "muxq_adapters"},
+    {"adapters_check", (PyCFunction)(void (*)(void))adapters_check, METH_FASTCALL, "muxq_adapters_check"},
     {"residual_norm", (PyCFunction)(void (*)(void))residual_norm, METH_FASTCALL, "muxq_residual_norm"},
     {"stream", stream, METH_NOARGS, "handle of the current stream"},
     {NULL, NULL, 0, NULL}};

@@ -527,3 +527,129 @@ def test_offsets_beyond_32_bits(gpu):
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     Y = mx.muxq_adapters(v["X"], v["A"], v["B"], v["ids"], status, v["scale"], None, v["base"])
     check(Y, *reference(v["X"], v["A"], v["B"], v["ids"], v["scale"], None, v["base"]))
+
+
+# ------------------------------------------------------------------------------------------------ beside muxq_linear
+class _Operand(FakeTensor):
+    is_cuda = True
+
+    def __init__(self, *a, at=0x100000, **k):
+        super().__init__(*a, **k)
+        self.at = at
+
+    def data_ptr(self):
+        return self.at
+
+    def numel(self):
+        return int(torch.tensor(self.shape).prod())
+
+    def is_contiguous(self):
+        return True
+
+
+_LINEAR_FN = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_int,
+                              ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p)
+
+
+@pytest.fixture
+def layer(mx):
+    """(muxq_linear with adapters on stand-ins for tensors, what was launched); the entry points are stand-ins too, but for the check"""
+    from paper_2604_04701_b200 import binding
+    launched = []
+
+    @_LINEAR_FN
+    def linear(*a):
+        launched.append("linear")
+        return 0
+
+    @_FN
+    def adapters(*a):
+        launched.append("adapters")
+        return 0
+
+    L = mx.lib()
+    at = lambda f: ctypes.cast(f, ctypes.c_void_p).value
+    binding._calls.bind(at(linear), at(linear), at(linear), lambda: 0, lambda d: 0, F16, F32, at(adapters), at(adapters), torch.int32, at(L.muxq_adapters_check))
+    O = _Operand
+    i32 = torch.int32
+
+    def call(out_kind=None, **over):
+        v = dict(X=O((5, 64), at=0x100000), out=O((5, 128), at=0x600000), A=O((3, 16, 64), at=0x200000), B=O((3, 128, 16), at=0x300000), row_slot=O((5,), dtype=i32, at=0x400000),
+                 scale=O((3,), dtype=F32, at=0x410000), rank=O((3,), dtype=i32, at=0x420000))
+        v.update(over)
+        ws = type("Ws", (), dict(buf=O((4096,), dtype=torch.uint8), status=O((1,), dtype=i32, at=0x440000)))
+        return mx.muxq_linear(v["X"], O((128, 64), dtype=torch.int8), O((1,), dtype=F32), mx.MuxqParams(), ws, mx.MUXQ_OUT_F16 if out_kind is None else out_kind, out=v["out"],
+                              adapters=mx.Adapters(v["A"], v["B"], v["row_slot"], v["scale"], v["rank"]))
+
+    yield call, launched
+    binding._lib = binding._calls = None
+    mx.lib()
+
+
+def test_the_layer_runs_with_its_adapters_behind_it(layer):
+    call, launched = layer
+    call()
+    assert launched == ["linear", "adapters"]
+
+
+@pytest.mark.parametrize("over", [
+    dict(A=_Operand((3, 16, 72))), dict(B=_Operand((3, 120, 16))), dict(B=_Operand((2, 128, 16))), dict(A=_Operand((3, 16, 64), dtype=F32)), dict(A=_Operand((16, 64))),
+    dict(A=_Operand((3, 16, 64), device=1)), dict(row_slot=_Operand((4,), dtype=torch.int32)), dict(row_slot=_Operand((5,), dtype=torch.int64)), dict(scale=_Operand((2,), dtype=F32)),
+    dict(rank=_Operand((3,), dtype=torch.int64)), dict(out=_Operand((6, 128))),
+    dict(out=_Operand((5, 128), dtype=F32)), dict(out_kind=1),  # out is not of out_kind
+])
+def test_adapters_that_do_not_fit_are_refused_before_the_layer_runs(layer, over):
+    call, launched = layer
+    with pytest.raises(ValueError):
+        call(**over)
+    assert not launched
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(out=_Operand((5, 128), at=0x100000)), 1),  # over X
+    (dict(A=_Operand((3, 16, 64), (512, 64, 1), at=0x200000)), 1), (dict(A=_Operand((3, 16, 64), at=0x200008)), 2), (dict(out=_Operand((5, 128), (132, 1), at=0x600000)), 2),
+    (dict(A=_Operand((3, 12, 64), at=0x200000), B=_Operand((3, 128, 12), (2048, 16, 1), at=0x300000)), 2), (dict(out_kind=2), 1),
+])
+def test_adapters_that_the_library_refuses_are_refused_before_the_layer_runs(mx, layer, over, code):
+    call, launched = layer
+    with pytest.raises(mx.MuxqError) as e:
+        call(**over)
+    assert e.value.status == code and not launched
+
+
+def test_the_check_says_what_the_call_would(mx):
+    """muxq_adapters_check launches nothing: a call that would be taken can be asked about without a device."""
+    p = ctypes.c_void_p
+
+    def check(**over):
+        v = dict(Y=0x600000, ldy=128, K=64, ldbase=128)
+        v.update(over)
+        s = _CSet(0x200000, 0x300000, 64, 16, 1024, 2048, 0x410000, 0x420000, 3, 16)
+        return mx.lib().muxq_adapters_check(p(0x100000), 4, v["K"], 64, ctypes.byref(s), p(0x430000), 128, p(0x500000), v["ldbase"], p(v["Y"]), v["ldy"], 0, p(0x440000))
+
+    assert check() == mx.MUXQ_OK and check(Y=0x500000) == mx.MUXQ_OK
+    assert check(Y=0x500010) == check(ldbase=120) == check(Y=0x100000) == mx.MUXQ_ERR_INVALID_ARG
+    assert check(K=60) == check(ldy=132) == mx.MUXQ_ERR_UNSUPPORTED
+
+
+@pytest.mark.gpu
+def test_a_refused_layer_leaves_its_result_alone(gpu):
+    mx = gpu
+    gen = torch.Generator().manual_seed(1)
+    K, N, M = 256, 640, 16
+    p = mx.MuxqParams()
+    w_q, s_w = mx.muxq_quantize((torch.randn(K, N, generator=gen) * 0.03).half().cuda(), p, True, mx.Workspace(mx.muxq_small_workspace_bytes(N)))
+    ws = mx.Workspace(mx.muxq_workspace_bytes(M, K, N, p))
+    v, whole = _inputs(M, K, N, 3, 16, None, F16)
+    out = whole[:M]
+    before = out.clone()
+    good = mx.Adapters(v["A"], v["B"], v["ids"], v["scale"])
+    for bad, error in ((good._replace(A=v["A"][:, :8]), ValueError), (good._replace(row_slot=v["ids"][:5]), ValueError), (good._replace(B=v["B"][:, :128]), ValueError)):
+        with pytest.raises(error):
+            mx.muxq_linear(v["X"], w_q, s_w, p, ws, mx.MUXQ_OUT_F16, out=out, adapters=bad)
+        torch.cuda.synchronize()
+        assert torch.equal(out, before)
+    alone = mx.muxq_linear(v["X"], w_q, s_w, p, ws, mx.MUXQ_OUT_F16)
+    mx.muxq_linear(v["X"], w_q, s_w, p, ws, mx.MUXQ_OUT_F16, out=out, adapters=good)
+    assert mx.muxq_read_status(ws) == mx.MUXQ_OK
+    check(out, *reference(v["X"], v["A"], v["B"], v["ids"], v["scale"], None, alone))
