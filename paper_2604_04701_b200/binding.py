@@ -112,6 +112,10 @@ def lib() -> ctypes.CDLL:
         L.muxq_read_status.argtypes = [vp, vp]; L.muxq_read_status.restype = i
         L.muxq_status_string.argtypes = [i]; L.muxq_status_string.restype = ctypes.c_char_p
         from . import _calls as calls
+        from . import build
+        has, wanted = getattr(calls, "built_for", "_calls.so of an earlier build"), build.MARK + build.built_for()
+        if has != wanted:  # it would read tensors by another torch's layout
+            raise RuntimeError(f"found {has}, wanted {wanted}: build it again with `python -m paper_2604_04701_b200.build`")
         at = lambda entry: ctypes.cast(entry, vp).value
         calls.bind(at(L.muxq_linear), at(L.muxq_linear_bias), at(L.muxq_quantize), torch._C._cuda_getDevice,
                    torch._C._cuda_getCurrentRawStream, torch.float16, torch.float32, at(L.muxq_residual_norm),

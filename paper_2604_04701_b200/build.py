@@ -31,11 +31,27 @@ def _deps_mtime():
     return max(os.path.getmtime(p) for p in paths)
 
 
+MARK = "_calls.so for "
+
+
+def built_for() -> str:
+    """What _calls.so depends on beside its sources: it reads tensors by the layout of the torch that it was compiled against."""
+    import torch
+    return f"{sys.implementation.cache_tag} torch {torch.__version__} {torch.version.git_version} abi {int(torch.compiled_with_cxx11_abi())}"
+
+
+def _calls_suit() -> bool:
+    """Whether _calls.so, which says so in a string of its own, was built for this Python and this torch (not by importing it)."""
+    with open(CALLS, "rb") as f:
+        return (MARK + built_for()).encode() + b"\0" in f.read()
+
+
 def build_calls() -> None:
     """_calls.so: py_calls.c, and py_tensor.cpp against the headers and libraries of the torch that is installed."""
     import torch
+    os.makedirs(OBJ_DIR, exist_ok=True)
     home = os.path.dirname(torch.__file__)
-    flags = ["-O2", "-Wall", "-fPIC", "-I" + sysconfig.get_paths()["include"]]
+    flags = ["-O2", "-Wall", "-fPIC", "-I" + sysconfig.get_paths()["include"], f'-DCALLS_BUILT_FOR="{MARK}{built_for()}"']
     objs = [os.path.join(OBJ_DIR, f) for f in ("py_calls.o", "py_tensor.o")]
     subprocess.check_call([os.environ.get("CC", "gcc"), *flags, "-c", os.path.join(CSRC, "py_calls.c"), "-o", objs[0]])
     cxx = os.environ.get("CXX", "g++")
@@ -49,10 +65,12 @@ def build_calls() -> None:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and all(os.path.exists(f) and os.path.getmtime(f) >= _deps_mtime() for f in (LIB, CALLS)):
+    fresh = lambda f: not force and os.path.exists(f) and os.path.getmtime(f) >= _deps_mtime()
+    if not fresh(CALLS) or not _calls_suit():
+        build_calls()
+    if fresh(LIB):
         return LIB
     os.makedirs(OBJ_DIR, exist_ok=True)
-    build_calls()
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     srcs = _sources()
     objs = [os.path.join(OBJ_DIR, os.path.basename(s)[:-3] + ".o") for s in srcs]

@@ -420,5 +420,10 @@ PyMODINIT_FUNC PyInit__calls(void) {
         {&n_w_bits, "w_bits"}, {&n_gran, "gran"}, {&n_aux_scale, "aux_scale"}, {&n_max_outliers, "max_outliers"}};
     for (size_t i = 0; i < sizeof names / sizeof *names; ++i)
         if (!*names[i].to && !(*names[i].to = PyUnicode_InternFromString(names[i].name))) return NULL;
-    return PyModule_Create(&module);
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built_for", CALLS_BUILT_FOR)) { /* by the build: Python and torch that this was compiled against */
+        Py_DECREF(m);
+        return NULL;
+    }
+    return m;
 }

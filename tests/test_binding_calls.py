@@ -105,3 +105,34 @@ def test_linear_refuses_operands_without_dimensions(calls):
         with pytest.raises((AssertionError, IndexError)):
             c.linear(*_args(p, X=X))
     assert not seen
+
+
+def test_the_extension_is_rebuilt_for_another_torch(monkeypatch):
+    """It reads tensors by the layout of the torch that it was compiled against: another one than that makes it stale, whatever the
+    sources' times say, and the library alone stays as it is."""
+    from paper_2604_04701_b200 import build
+    build.build()
+    built = []
+    monkeypatch.setattr(build, "build_calls", lambda: built.append(build.built_for()))
+    build.build()
+    assert not built
+    here = build.built_for()
+    assert torch.__version__ in here
+    monkeypatch.setattr(torch, "__version__", "99.1")
+    build.build()
+    assert built == [here.replace(here.split()[2], "99.1")]
+
+
+def test_an_extension_for_another_torch_is_not_used(monkeypatch):
+    from paper_2604_04701_b200 import binding, build
+    build.build()
+    binding.lib()
+    try:
+        binding._lib = binding._calls = None
+        with monkeypatch.context() as m:
+            m.setattr(build, "built_for", lambda: "cpython-312 torch 99.1")
+            with pytest.raises(RuntimeError, match="99.1"):
+                binding.lib()
+            assert binding._lib is None and binding._calls is None
+    finally:
+        binding.lib()
