@@ -611,9 +611,10 @@ int muxq_adapters_check(const void *X, int M, int K, int ldx, const muxq_adapter
     const size_t last = (size_t)(set->slots - 1);
     const Span wa{set->A_f16, 1, 1, ((last ? last * set->stride_a : 0) + (size_t)(set->max_rank - 1) * set->lda + K) * 2};
     const Span wb{set->B_f16, 1, 1, ((last ? last * set->stride_b : 0) + (size_t)(N - 1) * set->ldb + set->max_rank) * 2};
-    const Span ids{row_slot, 1, 1, (size_t)M * 4}, sc{set->scale, 1, 1, (size_t)set->slots * 4}, rk{set->rank, 1, 1, (size_t)set->slots * 4};
+    const Span ids{row_slot, 1, 1, (size_t)M * 4}, sc{set->scale, 1, 1, (size_t)set->slots * 4}, rk{set->rank, 1, 1, (size_t)set->slots * 4},
+        status{dev_status, 1, 1, 4};
     if ((overlap(y, b) && !same_place(y, b)) || overlap(y, x) || overlap(y, wa) || overlap(y, wb) || overlap(y, ids) || overlap(y, sc) ||
-        overlap(y, rk))
+        overlap(y, rk) || overlap(y, status))
         return MUXQ_ERR_INVALID_ARG;
     return MUXQ_OK;
 }

@@ -94,6 +94,11 @@ def test_unsupported_shapes_are_refused(mx, over):
     assert _call(mx, **over) == mx.MUXQ_ERR_UNSUPPORTED
 
 
+@pytest.mark.parametrize("at", [0x600000, 0x600000 + 3 * 256 + 252, 0x600000 + 128])
+def test_a_status_word_inside_the_result_is_refused(mx, at):
+    assert _call(mx, status=at) == mx.MUXQ_ERR_INVALID_ARG
+
+
 class FakeTensor:
     def __init__(self, shape, stride=None, dtype=F16, device=0):
         self.shape, self.dtype, self._device = shape, dtype, device
