@@ -83,17 +83,21 @@ struct Span {
 Span span(const void *p, int rows, int cols, int ld, int kind) {
     return Span{p, (size_t)rows, (size_t)ld * out_elem_bytes(kind), (size_t)cols * out_elem_bytes(kind)};
 }
-// Whether two matrices share a byte.  Columns of one wider matrix that lie side by side do not; of two matrices with different
-// pitches whose ranges of addresses meet it is taken that they do.
+// Whether two matrices share a byte.  Columns of one wider matrix that lie side by side do not, whether one takes all of its rows, every
+// second one or a single one; of matrices whose ranges of addresses meet and whose pitches have nothing to do with each other it is taken that they do.
 bool overlap(const Span &a, const Span &b) {
     if (!a.at || !b.at) return false;
     const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.at), b0 = reinterpret_cast<uintptr_t>(b.at);
     const uintptr_t a1 = a0 + (a.rows - 1) * a.pitch + a.width, b1 = b0 + (b.rows - 1) * b.pitch + b.width;
     if (a1 <= b0 || b1 <= a0) return false;
-    if (a.pitch != b.pitch || !a.pitch) return true;
-    const size_t d = (size_t)(b0 > a0 ? b0 - a0 : a0 - b0) % a.pitch;  // the later one's column within the earlier one's rows
+    if (a.rows == 1 && b.rows == 1) return true;
+    const size_t pa = a.rows > 1 ? a.pitch : b.pitch, pb = b.rows > 1 ? b.pitch : a.pitch;  // (one row: as the other's)
+    const size_t p = pa < pb ? pa : pb, q = pa < pb ? pb : pa;
+    if (!p || q % p) return true;
+    // every row of either begins at the same place within the shorter pitch
+    const size_t d = (size_t)(b0 > a0 ? b0 - a0 : a0 - b0) % p;  // the later one's column within the earlier one's rows
     const size_t first = b0 > a0 ? a.width : b.width, second = b0 > a0 ? b.width : a.width;
-    return d < first || d + second > a.pitch;
+    return d < first || d + second > p;
 }
 bool same_place(const Span &a, const Span &b) { return a.at == b.at && a.pitch == b.pitch && a.width == b.width; }
 

@@ -658,3 +658,22 @@ def test_a_refused_layer_leaves_its_result_alone(gpu):
     mx.muxq_linear(v["X"], w_q, s_w, p, ws, mx.MUXQ_OUT_F16, out=out, adapters=good)
     assert mx.muxq_read_status(ws) == mx.MUXQ_OK
     check(out, *reference(v["X"], v["A"], v["B"], v["ids"], v["scale"], None, alone))
+
+
+def test_operands_beside_the_result_in_one_wider_matrix(mx):
+    """Columns that lie side by side do not overlap, be it those of every row, of every second one or of one."""
+    p = ctypes.c_void_p
+
+    def check(ldy=256, **over):  # Y: four rows of 256 bytes, 512 apart
+        v = dict(scale=0x410000, rank=0x420000, base=0x500000, ldbase=128, status=0x440000, X=0x100000, ldx=64)
+        v.update(over)
+        s = _CSet(0x200000, 0x300000, 64, 16, 1024, 2048, v["scale"], v["rank"], 3, 16)
+        return mx.lib().muxq_adapters_check(p(v["X"]), 4, 64, v["ldx"], ctypes.byref(s), p(0x430000), 128, p(v["base"]), v["ldbase"], p(0x600000), ldy, 0, p(v["status"]))
+
+    Y = 0x600000
+    for free in (dict(scale=Y + 256), dict(rank=Y + 500), dict(status=Y + 2 * 512 + 400), dict(base=Y + 256, ldbase=256), dict(base=Y + 256, ldbase=512), dict(base=Y + 512 + 256, ldbase=768),
+                 dict(X=Y + 256, ldx=1024), dict(X=Y - 128, ldx=256), dict(scale=Y + 3 * 512 + 256)):
+        assert check(**free) == mx.MUXQ_OK, free
+    for over in (dict(scale=Y + 248), dict(scale=Y + 504), dict(rank=Y + 512), dict(status=Y + 2 * 512 + 252), dict(base=Y + 240, ldbase=512), dict(base=Y + 272, ldbase=512),
+                 dict(base=Y + 256, ldbase=384), dict(X=Y + 240, ldx=1024), dict(X=Y - 112, ldx=256), dict(X=Y + 512 - 16, ldx=512)):
+        assert check(**over) == mx.MUXQ_ERR_INVALID_ARG, over

@@ -436,3 +436,20 @@ def test_weight_and_bias_each_alone(gpu, M, D, kind, weight, bias):
     h, e, x, ex = reference(R, Y, pre, post, None, 1, 0.7)
     check(H, F32, h, e, "h")
     check(X, F16, x, ex, "x")
+
+
+@pytest.mark.gpu
+def test_a_gate_beside_the_result_in_one_wider_matrix(gpu):
+    """The gate is a row, or every third row, of columns that lie beside X's."""
+    mx = gpu
+    gen = torch.Generator().manual_seed(9)
+    whole = torch.randn(66, 2 * 264, generator=gen).half().cuda()
+    R, Y = torch.randn(66, 264, generator=gen).cuda(), torch.randn(66, 264, generator=gen).half().cuda()
+    n, X = mx.Norm(RMS, _vec(gen, 264)), whole[:, :264]
+    right = whole[:, 264:].clone()
+    for gate, group in ((whole[7, 264:], 1), (whole[::3, 264:], 3)):
+        want = mx.muxq_residual_norm(R, Y, n, gate=gate.clone(), gate_group=group)
+        h, x = mx.muxq_residual_norm(R, Y, n, gate=gate, gate_group=group, X=X)
+        assert torch.equal(h, want[0]) and torch.equal(x, want[1]) and torch.equal(whole[:, 264:], right)
+    with pytest.raises(mx.MuxqError):
+        mx.muxq_residual_norm(R, Y, n, gate=whole[7, 256:520], X=X)
