@@ -308,11 +308,13 @@ def muxq_adapters(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, row_slot: t
     requests beside the projection they share.  A [slots, R, K] and B [slots, N, R] fp16, rank int32 [slots] (None: R everywhere;
     what lies beyond a slot's rank is not used), scale fp32 [slots] (None: 1).  base is the projection's result, fp16 or fp32 (None: 0), and may
     be `out`.  Y has the type of base, or out_kind.  status: device int32[1], raised on a slot or a rank out of range."""
+    if out_kind == MUXQ_OUT_ACC_I32:
+        raise MuxqError("muxq_adapters", MUXQ_ERR_INVALID_ARG)
     if out is None:
         kind = out_kind if out_kind is not None else MUXQ_OUT_F32 if base is not None and base.dtype == torch.float32 else MUXQ_OUT_F16
-        if kind == MUXQ_OUT_ACC_I32:
-            raise MuxqError("muxq_adapters", MUXQ_ERR_INVALID_ARG)
         out = _alloc_out(X.shape[0], B.shape[1], kind, X.device)
+    elif out_kind is not None and out.dtype != (torch.float32 if out_kind == MUXQ_OUT_F32 else torch.float16):
+        raise ValueError("out: the type of out_kind is wanted")
     rc = _hot().adapters(X, A, B, row_slot, scale, rank, base, out, status)
     if rc:
         raise MuxqError("muxq_adapters", rc)

@@ -677,3 +677,11 @@ def test_operands_beside_the_result_in_one_wider_matrix(mx):
     for over in (dict(scale=Y + 248), dict(scale=Y + 504), dict(rank=Y + 512), dict(status=Y + 2 * 512 + 252), dict(base=Y + 240, ldbase=512), dict(base=Y + 272, ldbase=512),
                  dict(base=Y + 256, ldbase=384), dict(X=Y + 240, ldx=1024), dict(X=Y - 112, ldx=256), dict(X=Y + 512 - 16, ldx=512)):
         assert check(**over) == mx.MUXQ_ERR_INVALID_ARG, over
+
+
+@pytest.mark.parametrize("dtype,out_kind", [(F32, 0), (F16, 1), (F16, 2), (torch.int32, 2)])
+def test_a_result_of_another_type_than_out_kind_is_refused(mx, dtype, out_kind):
+    t = lambda *s: torch.zeros(*s, dtype=F16)
+    with pytest.raises((ValueError, mx.MuxqError), match="out_kind|invalid"):
+        mx.muxq_adapters(t(5, 64), t(3, 16, 64), t(3, 128, 16), torch.zeros(5, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), out_kind=out_kind,
+                         out=torch.zeros(5, 128, dtype=dtype))
