@@ -217,15 +217,14 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
         if (ok) ok = mbar_wait_warp(&t_full, 0, abort_flag, p.spin);
         for (; issued_base < u1 - u0 && ok; ++issued_base)
             if (!load_base(issued_base)) { ok = false; break; }
-        if (!ok) {  // every copy that was started lands before the CTA ends
-            for (int k = issued_x > x_stages ? issued_x - x_stages : 0; k < issued_x; ++k)
-                if (k != p.skip_chunk)
-                    for (uint32_t i = 0; i < kSpinLimit; ++i)
-                        if (__all_sync(0xffffffffu, mbar_try_wait(&x_full[k % x_stages], (k / x_stages) & 1))) break;
-            for (int k = issued_base > kBaseStages ? issued_base - kBaseStages : 0; k < issued_base; ++k)
+        // Every copy that was started lands before the CTA ends, also where this warp was through with all of its own when another one gave up.
+        for (int k = issued_x > x_stages ? issued_x - x_stages : 0; k < issued_x; ++k)
+            if (k != p.skip_chunk)
                 for (uint32_t i = 0; i < kSpinLimit; ++i)
-                    if (__all_sync(0xffffffffu, mbar_try_wait(&base_full[k % kBaseStages], (k / kBaseStages) & 1))) break;
-        }
+                    if (__all_sync(0xffffffffu, mbar_try_wait(&x_full[k % x_stages], (k / x_stages) & 1))) break;
+        for (int k = issued_base > kBaseStages ? issued_base - kBaseStages : 0; k < issued_base; ++k)
+            for (uint32_t i = 0; i < kSpinLimit; ++i)
+                if (__all_sync(0xffffffffu, mbar_try_wait(&base_full[k % kBaseStages], (k / kBaseStages) & 1))) break;
     } else if (warp == kWarpB) {
         // ------------------------------------------------------------ B, one adapter's for G steps of N at a time
         const int all = (u1 - u0 + G - 1) / G * d;
@@ -254,16 +253,14 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
             if (s_win.uneven && issued) ok = even(issued - 1);
         }
         if (ok && s_win.uneven) ok = even(issued - 1);
-        if (!ok)
-            for (int k = issued > b_stages ? issued - b_stages : 0; k < issued; ++k)
-                for (uint32_t i = 0; i < kSpinLimit; ++i)
-                    if (__all_sync(0xffffffffu, mbar_try_wait(&b_full[k % b_stages], (k / b_stages) & 1))) break;
+        for (int k = issued > b_stages ? issued - b_stages : 0; k < issued; ++k)  // (as above)
+            for (uint32_t i = 0; i < kSpinLimit; ++i)
+                if (__all_sync(0xffffffffu, mbar_try_wait(&b_full[k % b_stages], (k / b_stages) & 1))) break;
     } else if (warp == 1) {
         // ------------------------------------------------------------ products
         // Addresses and descriptors have to be uniform to the compiler, too, or every instruction waits for several moves to uniform registers: they
         // are made of kernel arguments, loop counters and constants, and the number of adapters, which shared memory tells, is one of the latter.
         // All of tensor memory is ours, so it begins at 0.
-        bool ok = true;
         const uint32_t sm0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
         auto issue = [&](auto number) {
             constexpr int D = decltype(number)::value;
@@ -324,16 +321,14 @@ k_adapter_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant_
             return true;
         };
         switch (d) {
-            case 1: ok = issue(std::integral_constant<int, 1>{}); break;
-            case 2: ok = issue(std::integral_constant<int, 2>{}); break;
-            case 3: ok = issue(std::integral_constant<int, 3>{}); break;
-            default: ok = issue(std::integral_constant<int, 4>{}); break;
+            case 1: issue(std::integral_constant<int, 1>{}); break;
+            case 2: issue(std::integral_constant<int, 2>{}); break;
+            case 3: issue(std::integral_constant<int, 3>{}); break;
+            default: issue(std::integral_constant<int, 4>{}); break;
         }
-        if (!ok) {  // products that are on their way end before their memory is given back
-            mma_commit_elect(&drained);
-            for (uint32_t i = 0; i < kSpinLimit; ++i)
-                if (__all_sync(0xffffffffu, mbar_try_wait(&drained, 0))) break;
-        }
+        mma_commit_elect(&drained);  // products that are on their way end before their memory is given back
+        for (uint32_t i = 0; i < kSpinLimit; ++i)
+            if (__all_sync(0xffffffffu, mbar_try_wait(&drained, 0))) break;
     } else {
         // ------------------------------------------------------------ T, then the results
         const int quad = warp & 3, group = (warp - 2) >> 2, row = quad * 32 + lane;
