@@ -364,8 +364,9 @@ int muxq_residual_norm(const void *R, int ldr, int res_kind, const void *Y, int 
  *   dev_status  device int32 (sticky): raised to MUXQ_ERR_INVALID_ARG when a used row_slot or rank is out of range (the rows
  *         concerned are then taken as rows without an adapter), to MUXQ_ERR_TIMEOUT when a bounded wait expires (Y then unspecified)
  * Everything is read in stream order (an adapter may be loaded into a slot by work ahead of the call).  Y overlaps nothing but base;
- * rows behind M and columns behind N are left as they are.  Results do not depend on the other rows of the batch but for the order
- * of the sums over K, and are the same from call to call.  K, N, max_rank, pitches and strides are multiples of 8 (pitch of
+ * rows behind M and columns behind N are left as they are.  The other rows of the batch decide in which order a row's sums over K
+ * and over the ranks are made, and nothing else of its result; the same call gives the same bits.  A value of X that is not finite leaves
+ * its own row unspecified, one of A or B the rows of its slot.  K, N, max_rank, pitches and strides are multiples of 8 (pitch of
  * an fp32 matrix: 4), max_rank <= 128, X, A, B, base and Y 16-byte aligned.  No workspace.
  */
 typedef struct muxq_adapter_set {
