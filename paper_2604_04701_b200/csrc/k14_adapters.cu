@@ -15,7 +15,7 @@
 // Bound: one chain of latencies at decode steps -- row_slot, then X and A, the parts of T through the cluster, T B^T -- of about 6200 cycles
 // behind the wait for the launch before (1 x 768 -> 768 rank 8 in a row of calls 3.9 us, 16 x 1280 -> 3840 with 16 adapters 5.4); what shaped it, us of the first:
 // 64-bit divisions for a CTA's share of K and N 4.8 -> 4.1, parts of T pushed by stores instead of fetched behind the barrier and rows
-// ordered by one warp 5.9 -> 4.8.  Between, memory: 1003 x 1280 -> 5120 rank 32 20.9 us, its columns of N at 4.8 TB/s.
+// ordered by one warp 5.9 -> 4.8.  Between, memory: 1003 x 1280 -> 5120 rank 32 20.6 us, its columns of N at 4.8 TB/s.
 #include "../../include/muxq.h"
 #include "k14_adapters.cuh"
 
@@ -493,8 +493,9 @@ cudaError_t launch_form(const AdapterArgs &a, int sms, cudaStream_t s) {
             done.have[dev] = true;
         }
     }
-    // As many CTAs as the device holds two of on an SM: clusters of 8 as long as windows of up to 32 rows make few enough of them, then smaller
-    // ones.  Behind k_adapter_tiles windows of 128 rows, of 64 or 32 where those would leave SMs idle.
+    // Up to two CTAs for every SM: clusters of 8 as long as windows of up to 32 rows make few enough of them, then smaller ones.  An SM holds
+    // two up to rank 64; above, it holds one (registers; from windows of 16 rows shared memory too), and more CTAs than SMs run one behind the other.
+    // Behind k_adapter_tiles windows of 128 rows, of 64 or 32 where those would leave SMs idle.
     const auto windows = [&](int rows) { return ((long long)a.M + rows - 1) / rows; };
     const auto largest = [&](int rows) {  // cluster
         int l = 3;

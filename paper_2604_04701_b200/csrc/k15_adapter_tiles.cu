@@ -12,12 +12,15 @@
 //
 // Roles: warp 0 TMA for X, A, then base; warp 1 products; groups of four warps for the results (one per quarter of the tensor memory's
 // lanes, the first group also for T), steps of N dealt out in turn so that their chains of latencies overlap; the last warp TMA for B.
-// Every wait is bounded; on expiry the CTA raises MUXQ_ERR_TIMEOUT, lets its copies and products end and returns.
+// Every wait is bounded; on expiry the CTA raises MUXQ_ERR_TIMEOUT, lets the copies and products of all roles end and returns.
 //
-// Bound: HBM from some 8192 rows on (16384 x 1280 -> 5120 at rank 64: 69 us for 378 MB, 5.5 TB/s; the steps of N run at the rate of HBM, but
-// nothing of them overlaps the first product and T, which took 31 of 125 thousand cycles), below that the chain window - T - products
-// with few windows for the device.  Taken from 1024 rows on, k_adapters below, us, here / k_adapters: 1003 x 1280 -> 5120
-// rank 32 20.8 / 20.9, 900 x 2560 -> 2560 21.7 / 14.1, 700 x 1280 -> 1280 14.1 / 9.5; 8192 x 768 -> 2304 22.6 / 46, 16384 rows 73 / 179.
+// Bound: HBM from some 8192 rows on (16384 x 1280 -> 5120 at rank 64: 384 MB in 72 to 77 us a call, 5.0 to 5.3 TB/s, with the launch of k_adapters
+// behind it; this kernel's steps of N run at the rate of HBM, but nothing of them overlaps the first product and T, which took 31 of 125
+// thousand cycles), below that the chain window - T - products with few windows for the device.  Taken from 1024 rows on, k_adapters below.  Rows
+// alone decide, which suits high ranks and N longer than K and costs the others up to a half until some 2500 rows; us here / k_adapters, four adapters
+// in runs, fp16, at 1024, 2048, 3000 rows: 1280 -> 5120 rank 64 17.6 / 21.0, 22.7 / 28.1, 27.4 / 56.6; 768 -> 2304 rank 64 13.9 / 15.3, 15.2 / 17.4,
+// 17.6 / 31.5; 1280 -> 5120 rank 16 15.6 / 12.6, 18.9 / 19.3, 23.4 / 38.0; 2560 -> 2560 rank 16 20.8 / 10.6, 22.0 / 14.6, 25.2 / 28.4; 1280 -> 1280
+// rank 16 14.0 / 8.8, 14.5 / 9.3, 15.5 / 13.9; fp32 1003 x 1280 -> 5120 rank 32 20.8 / 20.9; 8192 x 768 -> 2304 22.6 / 46, 16384 rows 73 / 179.
 // Tried: clusters that divide K among the CTAs of a window and exchange T (the exchange costs 7000 cycles: 2000 rows 18.0 -> 19.6 us,
 // 8192 22.8 -> 26.2), eight stages of X instead of four (no change: a stage takes 600 cycles to be issued), three groups of result
 // warps (no change).
